@@ -24,7 +24,7 @@ BGPO_ERR_WORKSPACE = -2
 BGPO_ERR_HIP = -3
 BGPO_ERR_UNSUPPORTED = -4
 BGPO_ERR_BUDGET = -5
-BGPO_BF16, BGPO_F32 = 0, 1
+BGPO_BF16, BGPO_F32, BGPO_F64 = 0, 1, 2
 BGPO_T_IID = 0
 BGPO_T_STRATIFIED = 1
 BGPO_FLAG_NONFINITE = 1
@@ -48,6 +48,11 @@ class _PlanInfo(ctypes.Structure):
     _fields_ = [("samples_per_unit", ctypes.c_int32), ("dw_batch", ctypes.c_int32),
                 ("dx_splits", ctypes.c_int32), ("vocab_chunk", ctypes.c_int32),
                 ("workspace_bytes", ctypes.c_uint64), ("w_copy", ctypes.c_int32)]
+
+
+class _Logits(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("ld", ctypes.c_int64), ("V", ctypes.c_int32),
+                ("in_dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
 
 
 class Timing(ctypes.Structure):
@@ -88,6 +93,9 @@ def _load():
     lib.bgpo_moments_workspace_size.restype = sz
     lib.bgpo_moments_workspace_size.argtypes = []
     lib.bgpo_moments_summary.argtypes = [vp, vp, vp, ctypes.c_int64, i32, vp, vp, sz, vp]
+    lib.bgpo_logits_workspace_size.argtypes = [P(_Logits), P(sz)]
+    lib.bgpo_logits_logp.argtypes = [P(_Logits), vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.bgpo_logits_logp_bwd.argtypes = [P(_Logits), vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_int64, vp]
     lib.bgpo_test_gemm_nt.argtypes = [vp, vp, vp, i32, i32, i32, vp]
     lib.bgpo_test_gemm_split.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp]
     lib.bgpo_test_gemm_tn.argtypes = [vp, vp, vp, i32, i32, i32, vp]
@@ -99,6 +107,7 @@ def _load():
     for f in ("bgpo_workspace_size", "bgpo_workspace_plan", "bgpo_sample_masks", "bgpo_elbo_fwd",
               "bgpo_elbo_bwd_accumulate", "bgpo_elbo_bwd_accumulate_noalloc", "bgpo_elbo_fwd_rmsnorm",
               "bgpo_elbo_bwd_accumulate_rmsnorm", "bgpo_moments_update", "bgpo_moments_summary",
+              "bgpo_logits_workspace_size", "bgpo_logits_logp", "bgpo_logits_logp_bwd",
               "bgpo_test_gemm_nt", "bgpo_test_gemm_split", "bgpo_test_gemm_tn",
               "bgpo_test_gemm", "bgpo_test_gemm_pair",
               "bgpo_test_mask_multiblock"):
@@ -381,6 +390,113 @@ def bgpo_moments_summary(mean, m2, ref, count: int, out, workspace, stream=None)
                                      _ptr(out, "out", (torch.float64,), (3,)),
                                      _ptr(workspace, "workspace", (torch.uint8,)), workspace.numel(),
                                      _stream(stream)), "bgpo_moments_summary")
+
+
+_F32 = (torch.float32,)
+_U8 = (torch.uint8, torch.bool)
+
+
+def _on_current_device(t, name: str):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is on another device than the current one")
+
+
+def _vec(t: Optional[torch.Tensor], name: str, dtypes, n, allow_none=False):
+    """The address of a contiguous tensor of n elements on the current device."""
+    if t is None:
+        if allow_none:
+            return None
+        raise ValueError(f"{name} is required")
+    _on_current_device(t, name)
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected one of {dtypes}")
+    if t.dim() != 1 or t.shape[0] != n:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(n,)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _mat(t: Optional[torch.Tensor], name: str, dtypes, rows: int, cols: int, allow_none=False):
+    """(address, elements between rows) of a matrix with contiguous rows on the
+    current device."""
+    if t is None:
+        if allow_none:
+            return None, 0
+        raise ValueError(f"{name} is required")
+    _on_current_device(t, name)
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected one of {dtypes}")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(rows, cols)}")
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    if ld < cols:
+        if rows > 1:
+            raise ValueError(f"the rows of {name} overlap")
+        ld = cols
+    return t.data_ptr(), ld
+
+
+def _workspace_args(ws: Optional[torch.Tensor]):
+    """(address, bytes) of a workspace; None is one of no bytes."""
+    if ws is None:
+        return None, 0
+    return _vec(ws, "workspace", (torch.uint8,), ws.numel()), ws.numel()
+
+
+def _logits_problem(logits, scale: float, name="logits"):
+    if logits.dim() != 2:
+        raise ValueError(f"{name} must be a matrix [rows, V]")
+    rows, V = logits.shape
+    if rows == 0 or V == 0:
+        ld = V
+    else:
+        _, ld = _mat(logits, name, (torch.bfloat16, torch.float32), rows, V)
+    return _Logits(rows, ld, V, BGPO_F32 if logits.dtype == torch.float32 else BGPO_BF16, scale, 0)
+
+
+def bgpo_logits_workspace_size(rows: int, V: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.bgpo_logits_workspace_size(ctypes.byref(_Logits(rows, V, V, BGPO_BF16, 1.0, 0)), ctypes.byref(n)),
+           "bgpo_logits_workspace_size")
+    return int(n.value)
+
+
+def logits_workspace(rows: int, V: int, device="cuda") -> torch.Tensor:
+    """A caller-owned workspace of bgpo_logits_workspace_size() bytes."""
+    return torch.empty(bgpo_logits_workspace_size(rows, V), dtype=torch.uint8, device=device)
+
+
+def bgpo_logits_logp(logits, targets, logp, entropy=None, lse=None, workspace=None, row_mask=None, scale: float = 1.0,
+                     stream=None):
+    """Log-probability of each row's target (and the entropy and log-sum-exp)."""
+    prob = _logits_problem(logits, scale)
+    n = prob.rows
+    ws, ws_bytes = _workspace_args(workspace)
+    _check(_lib.bgpo_logits_logp(
+        ctypes.byref(prob), logits.data_ptr(), _vec(targets, "targets", (torch.int32,), n),
+        _vec(row_mask, "row_mask", _U8, n, allow_none=True), _vec(logp, "logp", _F32, n),
+        _vec(entropy, "entropy", _F32, n, allow_none=True), _vec(lse, "lse", _F32, n, allow_none=True),
+        ws, ws_bytes, _stream(stream)), "bgpo_logits_logp")
+
+
+def bgpo_logits_logp_bwd(logits, targets, lse, entropy, dlogp, dentropy, dlogits, row_mask=None, scale: float = 1.0,
+                         stream=None):
+    """Gradient of the logits from those of logp and the entropy; dlogits may be
+    logits itself."""
+    prob = _logits_problem(logits, scale)
+    n = prob.rows
+    out, ld_out = _mat(dlogits, "dlogits", (logits.dtype,), n, prob.V)
+    _check(_lib.bgpo_logits_logp_bwd(
+        ctypes.byref(prob), logits.data_ptr(), _vec(targets, "targets", (torch.int32,), n),
+        _vec(row_mask, "row_mask", _U8, n, allow_none=True), _vec(lse, "lse", _F32, n),
+        _vec(entropy, "entropy", _F32, n, allow_none=True), _vec(dlogp, "dlogp", _F32, n),
+        _vec(dentropy, "dentropy", _F32, n, allow_none=True), out, ld_out, _stream(stream)),
+        "bgpo_logits_logp_bwd")
 
 
 def bgpo_test_gemm_nt(A, B, C, stream=None):

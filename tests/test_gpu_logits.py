@@ -1,0 +1,281 @@
+"""Token log-probabilities of logits and their backward vs the float64 oracle.
+
+Tolerances count roundings.  Forward, per row: the exponents u = (x - m) c carry
+three roundings (2^-24 each, relative to |u|), so a term e^t is off by 3 |t| 2^-24
+and 2^-23 of the exponential itself, and the terms' mean |t| is at most ln V + 1
+(the entropy plus ln S); a thread sums V / 64 terms at most and joins 16 sums.
+lse and logp therefore lie within (V / 64 + 16 + 3 (ln V + 1) + 2) 2^-24, plus
+2^-23 of their own size (two roundings) and of x_y - m.  The entropy adds T / S,
+a sum of the same terms weighted with |t| <= 100: the same count times its size,
+at most ln V + 1, once more.  Backward, fp32: t = scale x - lse (2^-24 |t| absolute,
+|t| <= 104 where p > 0), two roundings of t log2e, the exponential, three
+products: p within (3 |t| + 6) 2^-24, the entropy's factor t + H likewise; bf16
+adds half a step, 2^-8 of the value.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import policy as oracle
+
+pytestmark = pytest.mark.gpu
+E24 = 2.0 ** -24
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def lib():
+    from paper_2510_11683_amd import bgpo
+    return bgpo
+
+
+def _make(rows, V, dtype, pad=0, seed=0, spread=3.0, offset=0):
+    """Logits [rows, V] inside a larger array, starting `offset` elements into it."""
+    rng = np.random.default_rng([seed, rows, V])
+    x = (spread * rng.standard_normal((rows, V))).astype(np.float32)
+    big = torch.full((rows * (V + pad) + offset,), 7.0, dtype=dtype, device="cuda")
+    v = big[offset:].view(rows, V + pad)[:, :V]
+    v.copy_(torch.from_numpy(x))
+    y = rng.integers(0, V, rows).astype(np.int32)
+    return v, v.float().cpu().numpy(), torch.from_numpy(y).cuda(), y
+
+
+def _fwd(x, y, mask=None, scale=1.0, entropy=True):
+    b = lib()
+    n, V = x.shape
+    f = lambda: torch.full((n,), 5.0, device="cuda")  # noqa: E731
+    logp, ent, lse = f(), f() if entropy else None, f()
+    b.bgpo_logits_logp(x, y, logp, ent, lse, b.logits_workspace(n, V), row_mask=mask, scale=scale)
+    return [None if t is None else t.cpu().numpy().astype(np.float64) for t in (logp, ent, lse)]
+
+
+def _fwd_tol(V):
+    n = (V / 64 + 16 + 3 * (math.log(V) + 1) + 2) * E24
+    return n, 2 * E24
+
+
+def _check_fwd(got, want, xf, yn, scale):
+    V = xf.shape[1]
+    n, rel = _fwd_tol(V)
+    with np.errstate(invalid="ignore"):
+        m = xf.max(1).astype(np.float64) - xf[np.arange(len(yn)), np.clip(yn, 0, V - 1)]
+    m = np.where(np.isfinite(m), m, 0.0) * scale
+    for g, w, weight in zip(got, want, (1.0, math.log(V) + 2, 1.0)):
+        if g is None:
+            continue
+        assert np.array_equal(np.isnan(g), np.isnan(w)), (g, w)
+        assert np.array_equal(np.isinf(g), np.isinf(w))
+        ok = np.isfinite(w)
+        err = np.abs(g[ok] - w[ok])
+        tol = n * weight + rel * (np.abs(w[ok]) + 2 * m[ok])
+        assert (err <= tol).all(), (err / tol).max()
+
+
+SHAPES = [(1, 1), (1, 2), (3, 7), (5, 8), (2, 9), (17, 64), (4, 255), (9, 256), (3, 1000), (66, 2051), (5, 8191),
+          (1, 32003), (7, 40001), (2, 126464), (300, 4097), (1100, 515), (3000, 66)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,V", SHAPES)
+def test_forward(rows, V, dtype):
+    for pad, offset, scale in ((0, 0, 1.0), (3, 1, 0.7)):
+        x, xf, y, yn = _make(rows, V, dtype, pad, offset=offset)
+        want = oracle.logits_logp(xf, yn, scale=np.float32(scale))
+        _check_fwd(_fwd(x, y, scale=scale), want, xf, yn, scale)
+        got = _fwd(x, y, scale=scale, entropy=False)
+        _check_fwd(got, want, xf, yn, scale)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [5, 70, 3001, 40000])
+def test_rows_at_their_limits(V, dtype):
+    """-inf, the type's lowest values, NaN, +inf, spikes, masked rows and targets
+    outside the vocabulary; every row beside ordinary ones."""
+    rows = 16
+    x, _, y, yn = _make(rows, V, dtype, pad=1)
+    low = torch.finfo(dtype).min
+    x[1, : V - 1] = -math.inf                 # one token is left
+    yn[1] = V - 1
+    x[2] = -math.inf                          # none
+    x[3, V // 2] = math.nan
+    x[4, 0] = math.inf
+    x[5] = low                                # the type's lowest everywhere: uniform
+    x[6, 1:] = low
+    yn[6] = 0
+    x[7] = math.nan                           # masked
+    x[8] = math.nan                           # negative target
+    yn[8] = -100
+    yn[9] = V                                 # past the vocabulary
+    yn[10] = 2 ** 31 - 1
+    x[11, V // 3] = 300.0                     # a sure token, drawn ...
+    yn[11] = V // 3
+    x[12, V // 3] = 300.0                     # ... and not drawn
+    yn[12] = V - 1
+    x[13, 0] = -math.inf                      # a target that cannot be drawn
+    yn[13] = 0
+    x[14] = -1e30
+    mask = np.ones(rows, np.uint8)
+    mask[7] = 0
+    y = torch.from_numpy(yn).cuda()
+    xf = x.float().cpu().numpy()
+    want = oracle.logits_logp(xf, yn, mask)
+    got = _fwd(x, y, torch.from_numpy(mask).cuda())
+    assert got[0][13] == -math.inf == want[0][13]
+    _check_fwd(got, want, xf, yn, 1.0)
+    for k in (7, 8):
+        assert all(g[k] == 0 for g in got)
+    # the backward of the same rows
+    rng = np.random.default_rng(V)
+    a, c = rng.standard_normal(rows), rng.standard_normal(rows)
+    a[15], c[15] = 0.0, 0.0
+    x[15] = math.nan                          # no gradient: not read
+    _check_bwd(x, y, yn, want, a, c, mask, 1.0, dtype)
+
+
+def _check_bwd(x, y, yn, stats, a, c, mask, scale, dtype, in_place=False, ld_pad=0):
+    b = lib()
+    n, V = x.shape
+    to = lambda v: torch.from_numpy(np.asarray(v, np.float32)).cuda()  # noqa: E731
+    lse, ent, a32 = to(stats[2]), to(stats[1]), to(a)
+    c32 = None if c is None else to(c)
+    xf = x.float().cpu().numpy()
+    big = torch.full((n, V + ld_pad), 9.0, dtype=dtype, device="cuda")
+    out = x if in_place else big[:, :V]
+    m = None if mask is None else torch.from_numpy(mask).cuda()
+    want = oracle.logits_logp_bwd(xf, yn, lse.cpu().numpy(), ent.cpu().numpy(), a32.cpu().numpy(),
+                                  None if c is None else c32.cpu().numpy(), mask, np.float32(scale))
+    b.bgpo_logits_logp_bwd(x, y, lse, ent if c is not None else None, a32, c32, out, row_mask=m, scale=scale)
+    got = out.float().cpu().numpy().astype(np.float64)
+    assert (big[:, V:] == 9.0).all()
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    with np.errstate(invalid="ignore", over="ignore"):
+        t = np.clip(xf.astype(np.float64) * scale - lse.cpu().numpy()[:, None].astype(np.float64), -104.0, 104.0)
+        p = np.exp(t)
+        pe = p * (3 * np.abs(t) + 6) * E24
+        tol = np.abs(a32.cpu().numpy()[:, None]) * pe
+        if c is not None:
+            h = ent.cpu().numpy()[:, None].astype(np.float64)
+            tol = tol + np.abs(c32.cpu().numpy()[:, None]) * (pe * np.abs(t + h) + 4 * p * (np.abs(t) + np.abs(h)) * E24)
+    tol = scale * tol + np.abs(want) * (4 * E24 + (2.0 ** -8 if dtype == torch.bfloat16 else 0.0))
+    # a target's entry is a difference a - a p; exponentials below the normal range count as 0
+    rows = np.arange(n)
+    ok = (yn >= 0) & (yn < V)
+    tol[rows[ok], yn[ok]] += 4 * E24 * scale * np.abs(a32.cpu().numpy()[ok])
+    tol += 2.0 ** -126 * 128 * scale * (np.abs(a32.cpu().numpy()[:, None]) + (0 if c is None else np.abs(c32.cpu().numpy()[:, None])))
+    tol = np.nan_to_num(tol, nan=0.0)        # (rows whose NaN are not to be read: exactly 0)
+    fin = np.isfinite(want)
+    err = np.abs(got - want)
+    assert (err[fin] <= tol[fin]).all(), (np.where(fin, err / tol, 0).max(), np.argwhere(fin & (err > tol))[:4])
+    return got
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,V", [s for s in SHAPES if s[0] * s[1] < 600_000])
+def test_backward(rows, V, dtype):
+    rng = np.random.default_rng([3, rows, V])
+    for pad, offset, scale, ent, ld_pad, in_place in ((0, 0, 1.0, False, 0, False), (5, 1, 1.3, True, 2, False),
+                                                      (1, 0, 0.6, True, 0, True)):
+        x, xf, y, yn = _make(rows, V, dtype, pad, offset=offset)
+        mask = (rng.random(rows) > 0.2).astype(np.uint8)
+        stats = oracle.logits_logp(xf, yn, scale=np.float32(scale))
+        a = rng.standard_normal(rows) * (rng.random(rows) > 0.2)
+        c = rng.standard_normal(rows) * (a != 0) if ent else None
+        _check_bwd(x, y, yn, stats, a, c, mask, scale, dtype, in_place, ld_pad)
+
+
+def test_backward_against_differences():
+    """The kernels' own gradient against central differences of the kernels' own
+    forward (fp32 logits, a step of 2^-5: the truncation is h^2 / 6 of a third
+    derivative below 1, 1.7e-4; the rounding of two sums of 6 rows 1e-6 / h)."""
+    b = lib()
+    rows, V, h = 6, 37, 2.0 ** -5
+    x, xf, y, yn = _make(rows, V, torch.float32, spread=1.0)
+    rng = np.random.default_rng(5)
+    a, c = (torch.from_numpy(rng.standard_normal(rows).astype(np.float32)).cuda() for _ in range(2))
+    logp, ent, lse = (torch.empty(rows, device="cuda") for _ in range(3))
+    b.bgpo_logits_logp(x, y, logp, ent, lse, scale=0.9)
+    dx = torch.empty_like(x)
+    b.bgpo_logits_logp_bwd(x, y, lse, ent, a, c, dx, scale=0.9)
+
+    def value(z):
+        out = _fwd(z, y, scale=0.9)
+        return (a.cpu().numpy() * out[0] + c.cpu().numpy() * out[1])
+
+    for v in range(V):
+        up, down = x.clone(), x.clone()
+        up[:, v] += h
+        down[:, v] -= h
+        fd = (value(up) - value(down)) / (2 * h)
+        assert np.abs(fd - dx[:, v].cpu().numpy()).max() <= (np.abs(a.cpu().numpy()).max() + 4 * np.abs(c.cpu().numpy()).max()) * 3e-4
+
+
+def test_calls_are_deterministic_and_replay():
+    """Two calls give the same bits; so do replays of a captured graph on new
+    logits in the same buffers, with eager work between them."""
+    b = lib()
+    for rows, V in ((3, 126464), (700, 5003)):
+        x, _, y, _ = _make(rows, V, torch.bfloat16)
+        logp, ent, lse = (torch.empty(rows, device="cuda") for _ in range(3))
+        dx = torch.empty_like(x)
+        a = torch.ones(rows, device="cuda")
+        ws = b.logits_workspace(rows, V)
+
+        def step():
+            b.bgpo_logits_logp(x, y, logp, ent, lse, ws)
+            b.bgpo_logits_logp_bwd(x, y, lse, ent, a, a, dx)
+
+        step()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step()
+        for k in range(3):
+            x.copy_(torch.randn(rows, V, device="cuda") * (k + 1))
+            outs = []
+            for run in (step, step, g.replay):
+                for t in (logp, ent, lse, dx):
+                    t.fill_(3.0)
+                ws.fill_(255)
+                run()
+                torch.cuda.synchronize()
+                outs.append([t.clone() for t in (logp, ent, lse, dx)])
+            for o in outs[1:]:
+                assert all(torch.equal(p, q) for p, q in zip(outs[0], o))
+
+
+def test_other_stream_and_empty_batches():
+    b = lib()
+    x, xf, y, yn = _make(40, 3001, torch.bfloat16)
+    s = torch.cuda.Stream()
+    logp = torch.full((40,), 2.0, device="cuda")
+    torch.cuda.synchronize()
+    b.bgpo_logits_logp(x, y, logp, workspace=b.logits_workspace(40, 3001), stream=s)
+    s.synchronize()
+    want = oracle.logits_logp(xf, yn)
+    _check_fwd([logp.cpu().numpy().astype(np.float64)], want[:1], xf, yn, 1.0)
+    none = torch.empty(0, device="cuda")
+    b.bgpo_logits_logp(x[:0], y[:0], none, none, none)
+    b.bgpo_logits_logp_bwd(x[:0], y[:0], none, None, none, None, x[:0])
+
+
+def test_large_offsets():
+    """Rows more than 2^32 bytes and elements into the array."""
+    b = lib()
+    rows, V, ld = 5, 513, (1 << 30) + 1
+    big = torch.empty(4 * ld + V, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(big, (rows, V), (ld, 1))
+    rng = np.random.default_rng(1)
+    xs = torch.from_numpy((2 * rng.standard_normal((rows, V))).astype(np.float32)).bfloat16()
+    x.copy_(xs)
+    yn = rng.integers(0, V, rows).astype(np.int32)
+    y = torch.from_numpy(yn).cuda()
+    want = oracle.logits_logp(xs.float().numpy(), yn)
+    got = _fwd(x, y)
+    _check_fwd(got, want, xs.float().numpy(), yn, 1.0)
+    _check_bwd(x, y, yn, want, rng.standard_normal(rows), rng.standard_normal(rows), None, 1.0, torch.bfloat16, in_place=True)
