@@ -1,10 +1,13 @@
 /*
- * bgpo_policy.h - token log-probabilities of logits (libbgpo).
+ * bgpo_policy.h - token log-probabilities and policy objectives (libbgpo).
  *
  * What stands beside the ELBO head of bgpo.h when a policy is trained or
  * scored: the log-probability of a given token in each row of logits that a
  * model has returned (an old policy, a reference model, a head with terms of
- * its own) with its backward pass.
+ * its own) with its backward pass; the clipped policy loss with a KL term on
+ * such log-probabilities, or on the ELBO estimates of bgpo_elbo_fwd; and the
+ * preference loss on paired log ratios, whose gradient goes back either to
+ * token log-probabilities or, as advantages, through the ELBO head.
  *
  * Conventions as in bgpo.h: array arguments are device pointers owned by the
  * caller, the problem structs host pointers; work is enqueued on `stream`
@@ -83,6 +86,144 @@ int bgpo_logits_logp_bwd(const bgpo_logits* prob, const void* logits, const int3
                          const uint8_t* row_mask, const float* lse, const float* entropy,
                          const float* dlogp, const float* dentropy, void* dlogits,
                          int64_t ld_out, void* stream);
+
+/* ---------------------------------------------------------------- policy loss */
+
+/* Element types of the objectives: BGPO_F32 of bgpo.h, and fp64 (the ELBO
+ * estimates of bgpo_elbo_fwd). */
+enum { BGPO_F64 = 2 };
+
+/* The ratio that is clipped, with d = logp - logp_old:
+ *   TOKEN     r = e^d of every token
+ *   SEQUENCE  r = exp(mean of d over the response's unmasked positions), one
+ *             ratio per response.  On the ELBO estimates ell[B, n_t] of
+ *             bgpo_elbo_fwd it is exp(B_theta - B_old) (Eq. elbo_ratio). */
+enum { BGPO_RATIO_TOKEN = 0, BGPO_RATIO_SEQUENCE = 1 };
+
+/* Weight of an unmasked position, n_b of them in response b, N in the batch. */
+enum {
+  BGPO_REDUCE_TOKENS = 0,     /* loss_scale / N */
+  BGPO_REDUCE_RESPONSES = 1,  /* loss_scale / n_b  (loss_scale 1/B: the mean over responses) */
+  BGPO_REDUCE_SUM = 2         /* loss_scale */
+};
+
+/* Estimators of KL(pi || pi_ref) at a position, q = logp_ref - logp. */
+enum {
+  BGPO_KL_K1 = 0,             /* -q */
+  BGPO_KL_K2 = 1,             /* q^2 / 2 */
+  BGPO_KL_K3 = 2              /* e^q - q - 1 */
+};
+
+typedef struct bgpo_policy {
+  int64_t ld_logp, ld_old, ld_ref, ld_mask, ld_dlogp;  /* elements between responses, >= L
+                                                          (any value for B = 1 or a NULL array) */
+  int64_t ld_adv;     /* 0: one advantage per response, adv[B]; >= L: per position, adv[B, L]
+                         (TOKEN ratio only) */
+  double clip_low;    /* 0 <= clip_low <= 1 */
+  double clip_high;   /* >= 0; INFINITY: not clipped from above */
+  double clip_dual;   /* 0: none, or > 1 */
+  double kl_coef;     /* finite */
+  double loss_scale;  /* finite */
+  int32_t B, L;       /* responses, positions; B L <= 2^40 */
+  int32_t dtype;      /* BGPO_F32 or BGPO_F64: logp, logp_old, logp_ref, dlogp */
+  int32_t ratio, reduce, kl;
+} bgpo_policy;
+
+/* Entries of the statistics (device double [BGPO_POLICY_STATS], overwritten);
+ * w is the position's weight above. */
+enum {
+  BGPO_POLICY_LOSS = 0,       /* [OBJECTIVE] + kl_coef [KL] */
+  BGPO_POLICY_OBJECTIVE = 1,  /* -sum w min(r A, clip(r) A) */
+  BGPO_POLICY_KL = 2,         /* sum w kl (0 without logp_ref) */
+  BGPO_POLICY_LOG_RATIO = 3,  /* sum w d */
+  BGPO_POLICY_TOKENS = 4,     /* N */
+  BGPO_POLICY_CUT = 5,        /* unmasked positions whose policy gradient the clip cuts off */
+  BGPO_POLICY_STATS = 6
+};
+
+int bgpo_policy_workspace_size(const bgpo_policy* prob, size_t* bytes);
+
+/* The clipped policy loss with a KL term, and its gradient.  Per position
+ *   f = min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A), and with clip_dual
+ *       c for A < 0: max(f, c A)
+ *   loss = sum w (-f + kl_coef kl)
+ *   dlogp = d loss / d logp  (written, not accumulated; 0 on masked positions)
+ * The policy gradient is cut off where the clamped term (or c A) is strictly
+ * the one taken.
+ *   logp      [B, L]  log-probabilities under the policy
+ *   logp_old  [B, L]  under the policy that drew the responses; NULL: d = 0
+ *   logp_ref  [B, L]  under the reference; NULL: no KL term (kl_coef must be 0)
+ *   adv       float [B] or [B, L] (ld_adv)
+ *   resp_mask uint8 [B, L]  positions that count; the others are not read
+ *   dlogp     [B, L]  out; NULL: the loss alone
+ *   stats     double [6]  out
+ *   status_flags  int32 [1]  |= BGPO_FLAG_NONFINITE if the loss or a gradient
+ *                 is not finite; may be NULL
+ * A response without unmasked positions contributes nothing.  With none in the
+ * whole batch every output is 0. */
+int bgpo_policy_loss(const bgpo_policy* prob, const void* logp, const void* logp_old,
+                     const void* logp_ref, const float* adv, const uint8_t* resp_mask,
+                     void* dlogp, double* stats, int32_t* status_flags, void* workspace,
+                     size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------- preference loss */
+
+/* Loss of a pair's margin m. */
+enum {
+  BGPO_PREF_SIGMOID = 0,      /* -(1 - e) log sigmoid(m) - e log sigmoid(-m), e = label_smoothing */
+  BGPO_PREF_HINGE = 1,        /* max(0, 1 - m) */
+  BGPO_PREF_SQUARED = 2       /* ((m - 1/2) / beta)^2 */
+};
+
+typedef struct bgpo_preference {
+  int64_t ld_win, ld_lose, ld_win_ref, ld_lose_ref, ld_win_mask, ld_lose_mask, ld_dwin,
+      ld_dlose;       /* elements between pairs, >= L (any value for P = 1 or a NULL array) */
+  int64_t adv_stride; /* elements between pairs of adv_win and adv_lose, >= 1 */
+  double beta;        /* > 0, finite */
+  double margin;      /* finite */
+  double label_smoothing;  /* 0 <= e < 1; 0 unless BGPO_PREF_SIGMOID */
+  double loss_scale;  /* finite; 1/P: the mean over pairs */
+  int32_t P, L;       /* pairs, positions; P L <= 2^39 */
+  int32_t dtype;      /* BGPO_F32 or BGPO_F64: the [P, L] arrays */
+  int32_t kind;       /* BGPO_PREF_* */
+  int32_t mean;       /* 0: a response's score is the sum over its unmasked positions,
+                         1: their mean (the ELBO estimate of bgpo_elbo_fwd's samples) */
+  int32_t reserved;   /* 0 */
+} bgpo_preference;
+
+/* Statistics (device double [3], overwritten): loss_scale times the sum of the
+ * pairs' losses, the number of pairs with m > 0, and the sum of m. */
+enum { BGPO_PREF_STATS = 3 };
+
+int bgpo_preference_workspace_size(const bgpo_preference* prob, size_t* bytes);
+
+/* The preference loss on paired log ratios, and its gradient.  With s(.) the
+ * sum or mean over a response's unmasked positions (0 if there are none),
+ *   m = beta ((s(win) - s(win_ref)) - (s(lose) - s(lose_ref))) - margin
+ *   win, lose           [P, L]  of the preferred and the other response of each
+ *                               pair: token log-probabilities, or samples l of
+ *                               the ELBO (L = n_t, no masks, mean = 1)
+ *   win_ref, lose_ref   [P, L]  the same under the reference; both or neither
+ *   win_mask, lose_mask uint8 [P, L]; both or neither (NULL: every position)
+ *   dwin, dlose         [P, L]  out: d loss / d win, d loss / d lose (written;
+ *                               0 on masked positions); both or neither
+ *   margins             double [P]  out: m; may be NULL
+ *   adv_win, adv_lose   float  out, adv_stride apart: -d loss / d s of each
+ *                               response; both or neither.  As `adv` of
+ *                               bgpo_elbo_bwd_accumulate with mean = 1,
+ *                               bound = BGPO_BOUND_TAYLOR and loss_scale 1
+ *                               they send this loss's gradient through the
+ *                               ELBO head
+ *   stats               double [3]  out
+ *   status_flags        as in bgpo_policy_loss (loss, or a response's
+ *                       gradient, not finite); may be NULL
+ * Pairs may interleave in one array (rows 2 p and 2 p + 1 with ld twice the
+ * row length), inputs and outputs alike. */
+int bgpo_preference_loss(const bgpo_preference* prob, const void* win, const void* lose,
+                         const void* win_ref, const void* lose_ref, const uint8_t* win_mask,
+                         const uint8_t* lose_mask, void* dwin, void* dlose, double* margins,
+                         float* adv_win, float* adv_lose, double* stats, int32_t* status_flags,
+                         void* workspace, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

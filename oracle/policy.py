@@ -49,3 +49,89 @@ def logits_logp_bwd(x, targets, lse, entropy, dlogp, dentropy=None, row_mask=Non
                 g[r] -= b * np.where(lp == -np.inf, 0.0, p * (lp + float(entropy[r])))
         g[r] *= scale
     return g
+
+
+# ---------------------------------------------------------------- policy loss
+
+def _clipped(r, A, lo, hi, dual):
+    """min(r A, clamp(r) A) with the second clip, and the derivative w.r.t. r."""
+    free, held = r * A, min(max(r, lo), hi) * A
+    f, df = (held, 0.0) if held < free else (free, A)
+    if dual and A < 0 and dual * A > f:
+        f, df = dual * A, 0.0
+    return f, df
+
+
+def policy_loss(logp, logp_old, logp_ref, adv, mask, ratio="token", reduce="tokens", kl="k3", clip_low=0.2, clip_high=0.2,
+                clip_dual=0.0, kl_coef=0.0, loss_scale=1.0):
+    """(statistics [6], dlogp [B, L], sum of |weighted terms|), position by position."""
+    B, L = logp.shape
+    on = np.asarray(mask) != 0
+    N = int(on.sum())
+    g = np.zeros((B, L))
+    stats = np.zeros(6)
+    size = 0.0
+    lo, hi = 1.0 - clip_low, 1.0 + clip_high
+    for b in range(B):
+        at = np.flatnonzero(on[b])
+        if not len(at):
+            continue
+        w = loss_scale / {"tokens": N, "responses": len(at), "sum": 1}[reduce]
+        lp = logp[b, at].astype(np.float64)
+        d = lp - logp_old[b, at].astype(np.float64) if logp_old is not None else np.zeros(len(at))
+        x = np.full(len(at), d.sum() / len(at)) if ratio == "sequence" else d
+        A = (adv[b, at] if np.ndim(adv) == 2 else np.full(len(at), adv[b])).astype(np.float64)
+        with np.errstate(over="ignore", invalid="ignore"):
+            r = np.exp(x)
+            f, df = (np.array(v) for v in zip(*(_clipped(ri, Ai, lo, hi, clip_dual) for ri, Ai in zip(r, A))))
+            gr = np.where(df != 0, -w * df * r, 0.0)
+        # in a sequence ratio every position moves the one ratio of all by 1 / n
+        g[b, at] = gr.sum() / len(at) if ratio == "sequence" else gr
+        k = np.zeros(len(at))
+        if logp_ref is not None:
+            q = logp_ref[b, at].astype(np.float64) - lp
+            k, dk = {"k1": (-q, np.ones_like(q)), "k2": (q * q / 2, -q), "k3": (np.expm1(q) - q, -np.expm1(q))}[kl]
+            g[b, at] += kl_coef * w * dk
+        stats[1] -= w * f.sum()
+        stats[2] += w * k.sum()
+        stats[3] += w * d.sum()
+        stats[4] += len(at)
+        stats[5] += ((df == 0) & (A != 0)).sum()
+        size += abs(w) * (np.abs(f).sum() + (1 + abs(kl_coef)) * np.abs(k).sum() + np.abs(d).sum())
+    stats[0] = stats[1] + kl_coef * stats[2]
+    return stats, g, size
+
+
+# ---------------------------------------------------------------- preference loss
+
+def preference_loss(win, lose, win_ref=None, lose_ref=None, win_mask=None, lose_mask=None, kind="sigmoid", mean=False,
+                    beta=0.1, margin=0.0, label_smoothing=0.0, loss_scale=1.0):
+    """dict(stats [3], margins [P], adv_win, adv_lose [P], dwin, dlose [P, L],
+    size: the sum of the magnitudes behind every margin)."""
+    P, L = win.shape
+    o = dict(stats=np.zeros(3), margins=np.zeros(P), adv_win=np.zeros(P), adv_lose=np.zeros(P), dwin=np.zeros((P, L)),
+             dlose=np.zeros((P, L)), size=np.zeros(P))
+    for p in range(P):
+        s, on = [], []
+        for x, ref, mask in ((win, win_ref, win_mask), (lose, lose_ref, lose_mask)):
+            at = np.arange(L) if mask is None else np.flatnonzero(mask[p])
+            v = x[p, at].astype(np.float64) - (0.0 if ref is None else ref[p, at].astype(np.float64))
+            n = max(len(at), 1) if mean else 1
+            s.append(v.sum() / n)
+            on.append((at, n))
+            o["size"][p] += beta * (np.abs(x[p, at]).astype(np.float64).sum() * 2) / n
+        m = beta * (s[0] - s[1]) - margin
+        if kind == "sigmoid":
+            e = label_smoothing
+            loss = (1 - e) * np.logaddexp(0.0, -m) + e * np.logaddexp(0.0, m)
+            dm = -(1 - e) * np.exp(-np.logaddexp(0.0, m)) + e * np.exp(-np.logaddexp(0.0, -m))
+        elif kind == "hinge":
+            loss, dm = max(0.0, 1.0 - m), -1.0 if m < 1 else 0.0
+        else:
+            loss, dm = ((m - 0.5) / beta) ** 2, 2 * (m - 0.5) / beta ** 2
+        ds = loss_scale * dm * beta
+        o["stats"] += loss_scale * loss, m > 0, m
+        o["margins"][p], o["adv_win"][p], o["adv_lose"][p] = m, -ds, ds
+        o["dwin"][p, on[0][0]] = ds / on[0][1]
+        o["dlose"][p, on[1][0]] = -ds / on[1][1]
+    return o

@@ -29,6 +29,14 @@ BGPO_T_IID = 0
 BGPO_T_STRATIFIED = 1
 BGPO_FLAG_NONFINITE = 1
 BGPO_BOUND_PAPER, BGPO_BOUND_TAYLOR, BGPO_BOUND_JENSEN, BGPO_BOUND_EXACT = 0, 1, 2, 3
+BGPO_RATIO_TOKEN, BGPO_RATIO_SEQUENCE = 0, 1
+BGPO_REDUCE_TOKENS, BGPO_REDUCE_RESPONSES, BGPO_REDUCE_SUM = 0, 1, 2
+BGPO_KL_K1, BGPO_KL_K2, BGPO_KL_K3 = 0, 1, 2
+BGPO_POLICY_LOSS, BGPO_POLICY_OBJECTIVE, BGPO_POLICY_KL = 0, 1, 2      # entries of the policy loss's statistics
+BGPO_POLICY_LOG_RATIO, BGPO_POLICY_TOKENS, BGPO_POLICY_CUT = 3, 4, 5
+BGPO_POLICY_STATS = 6
+BGPO_PREF_SIGMOID, BGPO_PREF_HINGE, BGPO_PREF_SQUARED = 0, 1, 2
+BGPO_PREF_STATS = 3
 KERNEL_CLASSES = ("transpose_w", "mask", "gather", "fwd", "ell", "softmax_grad", "dx", "dx_reduce", "dw",
                   "recompute")
 
@@ -53,6 +61,19 @@ class _PlanInfo(ctypes.Structure):
 class _Logits(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("ld", ctypes.c_int64), ("V", ctypes.c_int32),
                 ("in_dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class _Policy(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_int64) for k in ("ld_logp", "ld_old", "ld_ref", "ld_mask", "ld_dlogp", "ld_adv")] +
+                [(k, ctypes.c_double) for k in ("clip_low", "clip_high", "clip_dual", "kl_coef", "loss_scale")] +
+                [(k, ctypes.c_int32) for k in ("B", "L", "dtype", "ratio", "reduce", "kl")])
+
+
+class _Preference(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_int64) for k in ("ld_win", "ld_lose", "ld_win_ref", "ld_lose_ref", "ld_win_mask",
+                                               "ld_lose_mask", "ld_dwin", "ld_dlose", "adv_stride")] +
+                [(k, ctypes.c_double) for k in ("beta", "margin", "label_smoothing", "loss_scale")] +
+                [(k, ctypes.c_int32) for k in ("P", "L", "dtype", "kind", "mean", "reserved")])
 
 
 class Timing(ctypes.Structure):
@@ -96,6 +117,10 @@ def _load():
     lib.bgpo_logits_workspace_size.argtypes = [P(_Logits), P(sz)]
     lib.bgpo_logits_logp.argtypes = [P(_Logits), vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.bgpo_logits_logp_bwd.argtypes = [P(_Logits), vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_int64, vp]
+    lib.bgpo_policy_workspace_size.argtypes = [P(_Policy), P(sz)]
+    lib.bgpo_policy_loss.argtypes = [P(_Policy)] + [vp] * 9 + [sz, vp]
+    lib.bgpo_preference_workspace_size.argtypes = [P(_Preference), P(sz)]
+    lib.bgpo_preference_loss.argtypes = [P(_Preference)] + [vp] * 14 + [sz, vp]
     lib.bgpo_test_gemm_nt.argtypes = [vp, vp, vp, i32, i32, i32, vp]
     lib.bgpo_test_gemm_split.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp]
     lib.bgpo_test_gemm_tn.argtypes = [vp, vp, vp, i32, i32, i32, vp]
@@ -108,6 +133,8 @@ def _load():
               "bgpo_elbo_bwd_accumulate", "bgpo_elbo_bwd_accumulate_noalloc", "bgpo_elbo_fwd_rmsnorm",
               "bgpo_elbo_bwd_accumulate_rmsnorm", "bgpo_moments_update", "bgpo_moments_summary",
               "bgpo_logits_workspace_size", "bgpo_logits_logp", "bgpo_logits_logp_bwd",
+              "bgpo_policy_workspace_size", "bgpo_policy_loss", "bgpo_preference_workspace_size",
+              "bgpo_preference_loss",
               "bgpo_test_gemm_nt", "bgpo_test_gemm_split", "bgpo_test_gemm_tn",
               "bgpo_test_gemm", "bgpo_test_gemm_pair",
               "bgpo_test_mask_multiblock"):
@@ -497,6 +524,127 @@ def bgpo_logits_logp_bwd(logits, targets, lse, entropy, dlogp, dentropy, dlogits
         _vec(entropy, "entropy", _F32, n, allow_none=True), _vec(dlogp, "dlogp", _F32, n),
         _vec(dentropy, "dentropy", _F32, n, allow_none=True), out, ld_out, _stream(stream)),
         "bgpo_logits_logp_bwd")
+
+
+_FLOATS = (torch.float32, torch.float64)
+
+
+@dataclasses.dataclass
+class PolicyLoss:
+    """The settings of bgpo_policy (its strides and element type come from the
+    tensors of a call)."""
+    B: int
+    L: int
+    ratio: int = BGPO_RATIO_TOKEN
+    reduce: int = BGPO_REDUCE_TOKENS
+    clip_low: float = 0.2
+    clip_high: float = 0.2
+    clip_dual: float = 0.0        # 0: none
+    kl: int = BGPO_KL_K3
+    kl_coef: float = 0.0
+    loss_scale: float = 1.0
+
+    def c(self, ld=(0, 0, 0, 0, 0, 0), dtype=BGPO_F32) -> _Policy:
+        return _Policy(*ld, self.clip_low, self.clip_high, self.clip_dual, self.kl_coef, self.loss_scale, self.B,
+                       self.L, dtype, self.ratio, self.reduce, self.kl)
+
+
+def bgpo_policy_workspace_size(prob: PolicyLoss) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.bgpo_policy_workspace_size(ctypes.byref(prob.c()), ctypes.byref(n)), "bgpo_policy_workspace_size")
+    return int(n.value)
+
+
+def policy_workspace(prob: PolicyLoss, device="cuda") -> torch.Tensor:
+    """A caller-owned workspace of bgpo_policy_workspace_size() bytes."""
+    return torch.empty(bgpo_policy_workspace_size(prob), dtype=torch.uint8, device=device)
+
+
+def bgpo_policy_loss(prob: PolicyLoss, logp, logp_old, logp_ref, adv, resp_mask, dlogp, stats, workspace,
+                     status_flags=None, stream=None):
+    """Clipped policy loss with a KL term, and its gradient dlogp (None: the loss
+    alone); logp_old None: on-policy, logp_ref None: no KL term."""
+    B, L = prob.B, prob.L
+    lp, ld_logp = _mat(logp, "logp", _FLOATS, B, L)
+    t = (logp.dtype,)
+    old, ld_old = _mat(logp_old, "logp_old", t, B, L, allow_none=True)
+    ref, ld_ref = _mat(logp_ref, "logp_ref", t, B, L, allow_none=True)
+    mask, ld_mask = _mat(resp_mask, "resp_mask", _U8, B, L)
+    dl, ld_dlogp = _mat(dlogp, "dlogp", t, B, L, allow_none=True)
+    if adv is not None and adv.dim() == 2:
+        a, ld_adv = _mat(adv, "adv", _F32, B, L)
+    else:
+        a, ld_adv = _vec(adv, "adv", _F32, B), 0
+    ws, ws_bytes = _workspace_args(workspace)
+    _check(_lib.bgpo_policy_loss(
+        ctypes.byref(prob.c((ld_logp, ld_old, ld_ref, ld_mask, ld_dlogp, ld_adv),
+                            BGPO_F64 if logp.dtype == torch.float64 else BGPO_F32)),
+        lp, old, ref, a, mask, dl, _vec(stats, "stats", (torch.float64,), BGPO_POLICY_STATS),
+        _vec(status_flags, "status_flags", (torch.int32,), 1, allow_none=True), ws, ws_bytes, _stream(stream)),
+        "bgpo_policy_loss")
+
+
+@dataclasses.dataclass
+class PreferenceLoss:
+    """The settings of bgpo_preference (its strides and element type come from
+    the tensors of a call)."""
+    P: int
+    L: int
+    kind: int = BGPO_PREF_SIGMOID
+    mean: bool = False
+    beta: float = 0.1
+    margin: float = 0.0
+    label_smoothing: float = 0.0
+    loss_scale: float = 1.0
+
+    def c(self, ld=(0,) * 9, dtype=BGPO_F32) -> _Preference:
+        return _Preference(*ld, self.beta, self.margin, self.label_smoothing, self.loss_scale, self.P, self.L, dtype,
+                           self.kind, int(self.mean), 0)
+
+
+def bgpo_preference_workspace_size(prob: PreferenceLoss) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.bgpo_preference_workspace_size(ctypes.byref(prob.c()), ctypes.byref(n)),
+           "bgpo_preference_workspace_size")
+    return int(n.value)
+
+
+def preference_workspace(prob: PreferenceLoss, device="cuda") -> torch.Tensor:
+    """A caller-owned workspace of bgpo_preference_workspace_size() bytes."""
+    return torch.empty(bgpo_preference_workspace_size(prob), dtype=torch.uint8, device=device)
+
+
+def bgpo_preference_loss(prob: PreferenceLoss, win, lose, win_ref, lose_ref, win_mask, lose_mask, dwin, dlose, margins,
+                         adv_win, adv_lose, stats, workspace, status_flags=None, stream=None):
+    """Preference loss on paired log ratios and its gradient.  adv_win and
+    adv_lose (vectors of one stride) are the advantages that send it through
+    bgpo_elbo_bwd_accumulate with bound BGPO_BOUND_TAYLOR and loss scale 1."""
+    P, L = prob.P, prob.L
+    w, ld_w = _mat(win, "win", _FLOATS, P, L)
+    t = (win.dtype,)
+    lo, ld_lo = _mat(lose, "lose", t, P, L)
+    wr, ld_wr = _mat(win_ref, "win_ref", t, P, L, allow_none=True)
+    lr, ld_lr = _mat(lose_ref, "lose_ref", t, P, L, allow_none=True)
+    wm, ld_wm = _mat(win_mask, "win_mask", _U8, P, L, allow_none=True)
+    lm, ld_lm = _mat(lose_mask, "lose_mask", _U8, P, L, allow_none=True)
+    dw, ld_dw = _mat(dwin, "dwin", t, P, L, allow_none=True)
+    dl, ld_dl = _mat(dlose, "dlose", t, P, L, allow_none=True)
+    aw = al = None
+    stride = 1
+    if adv_win is not None or adv_lose is not None:
+        aw, al = (_mat(None if a is None else a[:, None] if a.dim() == 1 else a, name, _F32, P, 1, allow_none=True)
+                  for a, name in ((adv_win, "adv_win"), (adv_lose, "adv_lose")))
+        if P > 1 and None not in (aw[0], al[0]) and aw[1] != al[1]:
+            raise ValueError("adv_win and adv_lose have different strides")
+        stride, aw, al = aw[1], aw[0], al[0]
+    ws, ws_bytes = _workspace_args(workspace)
+    _check(_lib.bgpo_preference_loss(
+        ctypes.byref(prob.c((ld_w, ld_lo, ld_wr, ld_lr, ld_wm, ld_lm, ld_dw, ld_dl, stride),
+                            BGPO_F64 if win.dtype == torch.float64 else BGPO_F32)),
+        w, lo, wr, lr, wm, lm, dw, dl, _vec(margins, "margins", (torch.float64,), P, allow_none=True), aw, al,
+        _vec(stats, "stats", (torch.float64,), BGPO_PREF_STATS),
+        _vec(status_flags, "status_flags", (torch.int32,), 1, allow_none=True), ws, ws_bytes, _stream(stream)),
+        "bgpo_preference_loss")
 
 
 def bgpo_test_gemm_nt(A, B, C, stream=None):

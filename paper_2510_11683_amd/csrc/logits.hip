@@ -229,7 +229,7 @@ static int check_logits(const bgpo_logits* p) {
       (p->in_dtype != BGPO_BF16 && p->in_dtype != BGPO_F32))
     return BGPO_ERR_INVALID_ARG;
   if (p->rows >= int64_t(1) << 31 || p->V > 1 << 24) return BGPO_ERR_UNSUPPORTED;
-  if (p->rows > 1 && (p->ld < p->V || p->ld > int64_t(1) << 40)) return BGPO_ERR_INVALID_ARG;
+  if (bad_stride(p, p->ld, p->rows, p->V)) return BGPO_ERR_INVALID_ARG;
   return BGPO_OK;
 }
 
@@ -261,10 +261,10 @@ int bgpo_logits_logp(const bgpo_logits* prob, const void* logits, const int32_t*
   if (!logits || !targets || !logp) return BGPO_ERR_INVALID_ARG;
   const bool f32 = prob->in_dtype == BGPO_F32;
   const int64_t n = prob->rows, e = f32 ? 4 : 2;
-  const Span in[] = {rows_span(logits, n, prob->ld, prob->V, e), span(targets, n * 4), span(row_mask, n)};
-  const Span out[] = {span(logp, n * 4), span(entropy, n * 4), span(lse, n * 4)};
+  const Array in[] = {{logits, n, prob->ld, prob->V, e}, vec(targets, n, 4), vec(row_mask, n, 1)};
+  const Array out[] = {vec(logp, n, 4), vec(entropy, n, 4), vec(lse, n, 4)};
   if (misaligned(logits, e) || misaligned(targets, 4) || misaligned(logp, 4) || misaligned(entropy, 4) ||
-      misaligned(lse, 4) || any_overlap(out, 3, in, 3))
+      misaligned(lse, 4) || any_overlap(out, in))
     return BGPO_ERR_INVALID_ARG;
   const LogitRows p = logit_rows(prob, logits, targets, row_mask);
   const auto kernel = f32 ? (entropy ? k_logits_logp<float, true> : k_logits_logp<float, false>)
@@ -284,15 +284,15 @@ int bgpo_logits_logp_bwd(const bgpo_logits* prob, const void* logits, const int3
     return BGPO_ERR_INVALID_ARG;
   const bool f32 = prob->in_dtype == BGPO_F32;
   const int64_t n = prob->rows, e = f32 ? 4 : 2;
-  if (n > 1 && (ld_out < prob->V || ld_out > int64_t(1) << 40)) return BGPO_ERR_INVALID_ARG;
+  if (bad_stride(dlogits, ld_out, n, prob->V)) return BGPO_ERR_INVALID_ARG;
   const bool in_place = dlogits == logits && (n == 1 || ld_out == prob->ld);
-  const Span in[] = {in_place ? Span{0, 0} : rows_span(logits, n, prob->ld, prob->V, e),
-                     span(targets, n * 4), span(row_mask, n), span(lse, n * 4),
-                     span(dentropy ? entropy : nullptr, n * 4), span(dlogp, n * 4), span(dentropy, n * 4)};
-  const Span out[] = {rows_span(dlogits, n, ld_out, prob->V, e)};
+  const Array in[] = {{in_place ? nullptr : logits, n, prob->ld, prob->V, e}, vec(targets, n, 4),
+                      vec(row_mask, n, 1), vec(lse, n, 4), vec(dentropy ? entropy : nullptr, n, 4),
+                      vec(dlogp, n, 4), vec(dentropy, n, 4)};
+  const Array out[] = {{dlogits, n, ld_out, prob->V, e}};
   if (misaligned(logits, e) || misaligned(dlogits, e) || misaligned(targets, 4) || misaligned(lse, 4) ||
       misaligned(entropy, 4) || misaligned(dlogp, 4) || misaligned(dentropy, 4) ||
-      any_overlap(out, 1, in, 7))
+      any_overlap(out, in))
     return BGPO_ERR_INVALID_ARG;
   const LogitRows p = logit_rows(prob, logits, targets, row_mask);
   const int64_t ldo = n > 1 ? ld_out : 0;

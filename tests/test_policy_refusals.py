@@ -27,7 +27,7 @@ def test_exports_what_the_headers_declare(b):
     for h in ("bgpo_policy.h",):
         src = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", h)).read(), flags=re.S)
         names |= set(re.findall(r"\b(bgpo_\w+)\s*\(", src))
-    assert {"bgpo_logits_logp", "bgpo_logits_logp_bwd"} <= names
+    assert {"bgpo_logits_logp", "bgpo_policy_loss", "bgpo_preference_loss"} <= names
     for n in names:
         assert hasattr(b._lib, n), n
 
@@ -61,7 +61,7 @@ BAD_LOGITS = [(dict(rows=-1), INVALID), (dict(V=0), INVALID), (dict(V=-5), INVAL
               (dict(in_dtype=2), INVALID), (dict(in_dtype=-1), INVALID), (dict(scale=0.0), INVALID),
               (dict(scale=-1.0), INVALID), (dict(scale=math.nan), INVALID), (dict(scale=math.inf), INVALID),
               (dict(reserved=1), INVALID), (dict(rows=1 << 31), UNSUPPORTED),
-              (dict(V=(1 << 24) + 1, ld=1 << 25), UNSUPPORTED), (dict(ld=(1 << 40) + 1), INVALID)]
+              (dict(V=(1 << 24) + 1, ld=1 << 25), UNSUPPORTED), (dict(ld=(1 << 54) + 1), INVALID)]
 
 
 @pytest.mark.parametrize("kw,status", BAD_LOGITS)
@@ -105,6 +105,131 @@ def test_empty_batches_of_logits_are_done(b):
     p = _logits(b, rows=0)
     assert _logp(b, p, {i: None for i in range(6)}) == 0
     assert _logp_bwd(b, p, {i: None for i in range(8)}) == 0
+
+
+# ---------------------------------------------------------------- policy loss
+
+def _policy(b, B=4, L=100, ld=(128,) * 5 + (0,), dtype=1, **kw):
+    p = b.PolicyLoss(B, L).c(ld, dtype)
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+def _policy_loss(b, prob, over=()):
+    # logp, old, ref, adv, mask, dlogp, stats, flags, workspace
+    args = [at(k) for k in range(9)] + [1 << 30, None]
+    for i, v in dict(over).items():
+        args[i] = v
+    return b._lib.bgpo_policy_loss(ctypes.byref(prob) if prob is not None else None, *args)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(B=0), INVALID), (dict(L=0), INVALID), (dict(L=-3), INVALID), (dict(dtype=0), INVALID), (dict(dtype=3), INVALID),
+    (dict(ratio=2), INVALID), (dict(ratio=-1), INVALID), (dict(reduce=3), INVALID), (dict(reduce=-1), INVALID),
+    (dict(kl=3), INVALID), (dict(kl=-1), INVALID), (dict(clip_low=-0.1), INVALID), (dict(clip_low=1.1), INVALID),
+    (dict(clip_low=math.nan), INVALID), (dict(clip_high=-0.1), INVALID), (dict(clip_high=math.nan), INVALID),
+    (dict(clip_dual=1.0), INVALID), (dict(clip_dual=-2.0), INVALID), (dict(clip_dual=math.inf), INVALID),
+    (dict(kl_coef=math.nan), INVALID), (dict(loss_scale=math.inf), INVALID), (dict(ld_adv=-1), INVALID),
+    (dict(ratio=1, ld_adv=128), INVALID), (dict(B=1 << 21, L=1 << 20), UNSUPPORTED)])
+def test_policy_problems(b, kw, status):
+    n = ctypes.c_size_t(0)
+    p = _policy(b, **kw)
+    assert b._lib.bgpo_policy_workspace_size(ctypes.byref(p), ctypes.byref(n)) == status
+    assert _policy_loss(b, p) == status
+
+
+def test_policy_pointers(b):
+    n = ctypes.c_size_t(0)
+    assert b._lib.bgpo_policy_workspace_size(None, ctypes.byref(n)) == INVALID
+    assert b._lib.bgpo_policy_workspace_size(ctypes.byref(_policy(b)), None) == INVALID
+    assert b._lib.bgpo_policy_workspace_size(ctypes.byref(_policy(b)), ctypes.byref(n)) == 0
+    assert _policy_loss(b, None) == INVALID
+    for i in (0, 3, 4, 6):
+        assert _policy_loss(b, _policy(b), {i: None}) == INVALID
+    assert _policy_loss(b, _policy(b, kl_coef=0.1), {2: None}) == INVALID       # a KL term without a reference
+    for k in ("ld_logp", "ld_old", "ld_ref", "ld_mask", "ld_dlogp", "ld_adv"):
+        assert _policy_loss(b, _policy(b, **{k: 99})) == INVALID
+        assert _policy_loss(b, _policy(b, **{k: 1 << 55})) == INVALID
+    off = lambda k, m: ctypes.c_void_p(at(k).value + m)  # noqa: E731
+    for i in (0, 1, 2, 3, 5, 7):
+        assert _policy_loss(b, _policy(b), {i: off(i, 2)}) == INVALID
+    assert _policy_loss(b, _policy(b), {6: off(6, 4)}) == INVALID
+    for i in (0, 1, 2, 5):
+        assert _policy_loss(b, _policy(b, dtype=2), {i: off(i, 4)}) == INVALID
+    # the gradient in place of an input; the statistics in the last row's last bytes
+    for i in (0, 1, 2, 4):
+        assert _policy_loss(b, _policy(b), {5: at(i)}) == INVALID
+    assert _policy_loss(b, _policy(b), {5: at(3)}) == INVALID
+    assert _policy_loss(b, _policy(b), {6: off(0, 4 * (3 * 128 + 100) - 8)}) == INVALID
+    assert _policy_loss(b, _policy(b), {7: off(6, 40)}) == INVALID
+    for i, v in ((8, None), (8, off(8, 128)), (9, n.value - 1)):
+        assert _policy_loss(b, _policy(b), {i: v}) == WORKSPACE
+
+
+# ---------------------------------------------------------------- preference loss
+
+def _pref(b, P=4, L=100, ld=(128,) * 8 + (1,), dtype=1, **kw):
+    p = b.PreferenceLoss(P, L).c(ld, dtype)
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+def _pref_loss(b, prob, over=()):
+    # win, lose, their references, masks, gradients, margins, advantages, stats, flags, workspace
+    args = [at(k) for k in range(14)] + [1 << 30, None]
+    for i, v in dict(over).items():
+        args[i] = v
+    return b._lib.bgpo_preference_loss(ctypes.byref(prob) if prob is not None else None, *args)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(P=0), INVALID), (dict(L=0), INVALID), (dict(dtype=0), INVALID), (dict(dtype=3), INVALID), (dict(kind=3), INVALID),
+    (dict(kind=-1), INVALID), (dict(mean=2), INVALID), (dict(mean=-1), INVALID), (dict(reserved=1), INVALID),
+    (dict(beta=0.0), INVALID), (dict(beta=-1.0), INVALID), (dict(beta=math.inf), INVALID), (dict(beta=math.nan), INVALID),
+    (dict(margin=math.nan), INVALID), (dict(loss_scale=math.inf), INVALID), (dict(label_smoothing=-0.1), INVALID),
+    (dict(label_smoothing=1.0), INVALID), (dict(label_smoothing=0.1, kind=1), INVALID),
+    (dict(P=1 << 20, L=1 << 20), UNSUPPORTED)])
+def test_preference_problems(b, kw, status):
+    n = ctypes.c_size_t(0)
+    p = _pref(b, **kw)
+    assert b._lib.bgpo_preference_workspace_size(ctypes.byref(p), ctypes.byref(n)) == status
+    assert _pref_loss(b, p) == status
+
+
+def test_preference_pointers(b):
+    n = ctypes.c_size_t(0)
+    assert b._lib.bgpo_preference_workspace_size(None, ctypes.byref(n)) == INVALID
+    assert b._lib.bgpo_preference_workspace_size(ctypes.byref(_pref(b)), None) == INVALID
+    assert b._lib.bgpo_preference_workspace_size(ctypes.byref(_pref(b)), ctypes.byref(n)) == 0
+    assert _pref_loss(b, None) == INVALID
+    for i in (0, 1, 2, 3, 4, 5, 6, 7, 9, 10, 11):
+        assert _pref_loss(b, _pref(b), {i: None}) == INVALID
+    for k in ("ld_win", "ld_lose", "ld_win_ref", "ld_lose_ref", "ld_win_mask", "ld_lose_mask", "ld_dwin", "ld_dlose"):
+        assert _pref_loss(b, _pref(b, **{k: 99})) == INVALID
+    assert _pref_loss(b, _pref(b, adv_stride=0)) == INVALID
+    off = lambda k, m: ctypes.c_void_p(at(k).value + m)  # noqa: E731
+    for i in (0, 1, 2, 3, 6, 7, 9, 10, 12):
+        assert _pref_loss(b, _pref(b), {i: off(i, 2)}) == INVALID
+    for i in (8, 11):
+        assert _pref_loss(b, _pref(b), {i: off(i, 4)}) == INVALID
+    for out in (6, 7):
+        for i in range(6):
+            assert _pref_loss(b, _pref(b), {out: at(i)}) == INVALID
+    assert _pref_loss(b, _pref(b), {7: off(6, 4 * 50)}) == INVALID              # rows of the gradients overlap
+    assert _pref_loss(b, _pref(b, ld_dwin=256, ld_dlose=256), {7: off(6, 4 * 99)}) == INVALID
+    assert _pref_loss(b, _pref(b, ld_dwin=256, ld_dlose=256), {7: off(6, 4 * 157)}) == INVALID
+    assert _pref_loss(b, _pref(b), {10: at(9)}) == INVALID
+    assert _pref_loss(b, _pref(b, adv_stride=2), {10: off(9, 8)}) == INVALID
+    assert _pref_loss(b, _pref(b), {11: off(8, 24)}) == INVALID
+    # what interleaves without sharing a byte gets as far as the workspace
+    ok = {13: None}
+    assert _pref_loss(b, _pref(b, ld_dwin=256, ld_dlose=256), {7: off(6, 4 * 100), **ok}) == WORKSPACE
+    assert _pref_loss(b, _pref(b, ld_dwin=256, ld_dlose=256), {6: off(7, 4 * 156), **ok}) == WORKSPACE
+    assert _pref_loss(b, _pref(b, adv_stride=2), {10: off(9, 4), **ok}) == WORKSPACE
+    for i, v in ((13, None), (13, off(13, 128)), (14, n.value - 1)):
+        assert _pref_loss(b, _pref(b), {i: v}) == WORKSPACE
 
 
 def test_binding_refuses_tensors(b):
