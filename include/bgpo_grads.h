@@ -1,0 +1,65 @@
+/*
+ * bgpo_grads.h - norm of many gradients and their clipping (libbgpo).
+ *
+ * Between the backward pass (the dX and dW of bgpo.h, the gradients of the
+ * predictor's own parameters) and the optimiser: the norm of a list of tensors
+ * taken as one vector, and their scaling to a largest norm.
+ *
+ * Conventions as in bgpo.h.  The list is a HOST array, read before the call
+ * returns; its `data` are device pointers, aligned to their element type (16
+ * bytes is fastest).  Its entries travel in kernel arguments, so nothing is
+ * allocated or copied and the calls can be captured into a HIP graph, which
+ * then goes on using the addresses of the capture.
+ */
+#ifndef BGPO_GRADS_H_
+#define BGPO_GRADS_H_
+
+#include <stddef.h>
+#include <stdint.h>
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef struct bgpo_tensor {
+  void* data;
+  int64_t n;          /* elements, 0 <= n <= 2^38; data may be NULL for 0 */
+  int32_t dtype;      /* BGPO_BF16 or BGPO_F32 */
+  int32_t reserved;   /* 0 */
+} bgpo_tensor;
+
+enum {
+  BGPO_NORM_L2 = 0,   /* sqrt of the sum of squares */
+  BGPO_NORM_MAX = 1   /* largest magnitude */
+};
+
+/* Bytes of device workspace of bgpo_grad_norm (8-byte aligned). */
+size_t bgpo_grad_workspace_size(void);
+
+/* norm[0] (device double) = the norm over all entries of grads[count]; squares
+ * and sums in float64, in a fixed order (identical lists give identical bits).
+ * 0 for an empty list.  An entry that is in the list twice counts twice.
+ *   status_flags  int32 [1]  |= BGPO_FLAG_NONFINITE if the norm is not finite
+ *                 (a NaN or infinity anywhere); may be NULL */
+int bgpo_grad_norm(const bgpo_tensor* grads, int32_t count, int32_t norm_type, double* norm,
+                   int32_t* status_flags, void* workspace, size_t ws_bytes, void* stream);
+
+/* Scales every entry by max_norm / norm[0] where norm[0] > max_norm (in fp32,
+ * rounded once to the output's type).  norm is read on the device: the result
+ * of bgpo_grad_norm, or what a caller that holds only a shard has made of it.
+ *   max_norm  >= 0, finite
+ *   out       NULL: in place; nothing is read or written where no scaling is
+ *             due.  Else count entries of the same n: each is the scaled (or
+ *             plain) copy of its gradient, of its own dtype; an entry may be
+ *             its gradient itself (the same data and dtype).
+ * A norm that is not finite leaves the gradients as they are (copies them):
+ * the flag of bgpo_grad_norm tells the caller to drop the step.  An output
+ * must not overlap another entry of either list (BGPO_ERR_INVALID_ARG). */
+int bgpo_grad_clip(const bgpo_tensor* grads, const bgpo_tensor* out, int32_t count,
+                   double max_norm, const double* norm, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* BGPO_GRADS_H_ */

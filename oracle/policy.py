@@ -135,3 +135,17 @@ def preference_loss(win, lose, win_ref=None, lose_ref=None, win_mask=None, lose_
         o["dwin"][p, on[0][0]] = ds / on[0][1]
         o["dlose"][p, on[1][0]] = -ds / on[1][1]
     return o
+
+
+# ---------------------------------------------------------------- gradients
+
+def grad_norm(tensors, kind="l2"):
+    v = np.concatenate([np.asarray(t, dtype=np.float64).ravel() for t in tensors] or [np.zeros(0)])
+    if kind == "max":
+        return float(np.abs(v).max()) if v.size else 0.0
+    return float(np.sqrt(np.dot(v, v)))
+
+
+def grad_clip(tensors, max_norm, norm):
+    f = max_norm / norm if np.isfinite(norm) and norm > max_norm else 1.0
+    return [np.asarray(t, dtype=np.float64) * f for t in tensors]

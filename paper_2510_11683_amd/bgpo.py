@@ -37,6 +37,7 @@ BGPO_POLICY_LOG_RATIO, BGPO_POLICY_TOKENS, BGPO_POLICY_CUT = 3, 4, 5
 BGPO_POLICY_STATS = 6
 BGPO_PREF_SIGMOID, BGPO_PREF_HINGE, BGPO_PREF_SQUARED = 0, 1, 2
 BGPO_PREF_STATS = 3
+BGPO_NORM_L2, BGPO_NORM_MAX = 0, 1
 KERNEL_CLASSES = ("transpose_w", "mask", "gather", "fwd", "ell", "softmax_grad", "dx", "dx_reduce", "dw",
                   "recompute")
 
@@ -61,6 +62,10 @@ class _PlanInfo(ctypes.Structure):
 class _Logits(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("ld", ctypes.c_int64), ("V", ctypes.c_int32),
                 ("in_dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class _Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class _Policy(ctypes.Structure):
@@ -121,6 +126,10 @@ def _load():
     lib.bgpo_policy_loss.argtypes = [P(_Policy)] + [vp] * 9 + [sz, vp]
     lib.bgpo_preference_workspace_size.argtypes = [P(_Preference), P(sz)]
     lib.bgpo_preference_loss.argtypes = [P(_Preference)] + [vp] * 14 + [sz, vp]
+    lib.bgpo_grad_workspace_size.restype = sz
+    lib.bgpo_grad_workspace_size.argtypes = []
+    lib.bgpo_grad_norm.argtypes = [P(_Tensor), i32, i32, vp, vp, vp, sz, vp]
+    lib.bgpo_grad_clip.argtypes = [P(_Tensor), P(_Tensor), i32, ctypes.c_double, vp, vp]
     lib.bgpo_test_gemm_nt.argtypes = [vp, vp, vp, i32, i32, i32, vp]
     lib.bgpo_test_gemm_split.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp]
     lib.bgpo_test_gemm_tn.argtypes = [vp, vp, vp, i32, i32, i32, vp]
@@ -134,7 +143,7 @@ def _load():
               "bgpo_elbo_bwd_accumulate_rmsnorm", "bgpo_moments_update", "bgpo_moments_summary",
               "bgpo_logits_workspace_size", "bgpo_logits_logp", "bgpo_logits_logp_bwd",
               "bgpo_policy_workspace_size", "bgpo_policy_loss", "bgpo_preference_workspace_size",
-              "bgpo_preference_loss",
+              "bgpo_preference_loss", "bgpo_grad_norm", "bgpo_grad_clip",
               "bgpo_test_gemm_nt", "bgpo_test_gemm_split", "bgpo_test_gemm_tn",
               "bgpo_test_gemm", "bgpo_test_gemm_pair",
               "bgpo_test_mask_multiblock"):
@@ -645,6 +654,58 @@ def bgpo_preference_loss(prob: PreferenceLoss, win, lose, win_ref, lose_ref, win
         _vec(stats, "stats", (torch.float64,), BGPO_PREF_STATS),
         _vec(status_flags, "status_flags", (torch.int32,), 1, allow_none=True), ws, ws_bytes, _stream(stream)),
         "bgpo_preference_loss")
+
+
+class GradList:
+    """A list of gradients in the form that bgpo_grad_norm and bgpo_grad_clip
+    take; keeps the tensors.  Built once and used again: every call looks up
+    where the tensors are and how large."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        for i, t in enumerate(self.tensors):
+            _on_current_device(t, f"gradient {i}")
+            if t.dtype not in (torch.bfloat16, torch.float32):
+                raise ValueError(f"gradient {i} has dtype {t.dtype}, expected bfloat16 or float32")
+            if not t.is_contiguous():
+                raise ValueError(f"gradient {i} must be contiguous")
+        self._at = self._where()
+        self._c = (_Tensor * max(1, len(self.tensors)))(
+            *[_Tensor(t.data_ptr(), t.numel(), BGPO_F32 if t.dtype == torch.float32 else BGPO_BF16, 0)
+              for t in self.tensors])
+
+    def __len__(self):
+        return len(self.tensors)
+
+    def _where(self):
+        return [(t.data_ptr(), t.numel()) for t in self.tensors]
+
+    def c(self):
+        if self._at != self._where():
+            self.__init__(self.tensors)
+        return self._c
+
+
+def grad_workspace(device="cuda") -> torch.Tensor:
+    """A caller-owned workspace of bgpo_grad_workspace_size() bytes."""
+    return torch.empty(_lib.bgpo_grad_workspace_size(), dtype=torch.uint8, device=device)
+
+
+def bgpo_grad_norm(grads: GradList, norm, workspace, norm_type: int = BGPO_NORM_L2, status_flags=None, stream=None):
+    """norm[0] = the norm of all gradients of the list as one vector."""
+    ws, ws_bytes = _workspace_args(workspace)
+    _check(_lib.bgpo_grad_norm(grads.c(), len(grads), norm_type, _vec(norm, "norm", (torch.float64,), 1),
+                               _vec(status_flags, "status_flags", (torch.int32,), 1, allow_none=True), ws, ws_bytes,
+                               _stream(stream)), "bgpo_grad_norm")
+
+
+def bgpo_grad_clip(grads: GradList, max_norm: float, norm, out: Optional[GradList] = None, stream=None):
+    """Scales the gradients to a norm of max_norm where norm[0] is larger: in
+    place, or into the tensors of `out`."""
+    if out is not None and len(out) != len(grads):
+        raise ValueError(f"out has {len(out)} tensors, expected {len(grads)}")
+    _check(_lib.bgpo_grad_clip(grads.c(), None if out is None else out.c(), len(grads), float(max_norm),
+                               _vec(norm, "norm", (torch.float64,), 1), _stream(stream)), "bgpo_grad_clip")
 
 
 def bgpo_test_gemm_nt(A, B, C, stream=None):

@@ -24,10 +24,10 @@ def b():
 
 def test_exports_what_the_headers_declare(b):
     names = set()
-    for h in ("bgpo_policy.h",):
+    for h in ("bgpo_policy.h", "bgpo_grads.h"):
         src = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", h)).read(), flags=re.S)
         names |= set(re.findall(r"\b(bgpo_\w+)\s*\(", src))
-    assert {"bgpo_logits_logp", "bgpo_policy_loss", "bgpo_preference_loss"} <= names
+    assert {"bgpo_logits_logp", "bgpo_policy_loss", "bgpo_preference_loss", "bgpo_grad_norm", "bgpo_grad_clip"} <= names
     for n in names:
         assert hasattr(b._lib, n), n
 
@@ -232,6 +232,59 @@ def test_preference_pointers(b):
         assert _pref_loss(b, _pref(b), {i: v}) == WORKSPACE
 
 
+# ---------------------------------------------------------------- gradients
+
+def _list(b, *entries):
+    return (b._Tensor * max(1, len(entries)))(*[b._Tensor(*e) for e in entries])
+
+
+BAD_ENTRIES = [((1 << 44, -1, 1, 0), INVALID), ((None, 4, 1, 0), INVALID), ((1 << 44, 4, 2, 0), INVALID),
+               ((1 << 44, 4, -1, 0), INVALID), ((1 << 44, 4, 1, 1), INVALID), (((1 << 44) + 2, 4, 1, 0), INVALID),
+               (((1 << 44) + 1, 4, 0, 0), INVALID), ((1 << 44, (1 << 38) + 1, 1, 0), UNSUPPORTED)]
+
+
+@pytest.mark.parametrize("entry,status", BAD_ENTRIES)
+def test_gradient_entries(b, entry, status):
+    g = _list(b, (1 << 45, 8, 1, 0), entry)
+    n = b._lib.bgpo_grad_workspace_size()
+    assert b._lib.bgpo_grad_norm(g, 2, 0, at(3), None, at(4), n, None) == status
+    assert b._lib.bgpo_grad_clip(g, None, 2, 1.0, at(3), None) == status
+    ok = _list(b, (1 << 46, 8, 1, 0), (1 << 47, 4, 1, 0))
+    assert b._lib.bgpo_grad_clip(ok, g, 2, 1.0, at(3), None) == status
+
+
+def test_gradient_arguments(b):
+    g = _list(b, (1 << 45, 8, 1, 0), (1 << 46, 8, 0, 0))
+    n = b._lib.bgpo_grad_workspace_size()
+    norm = b._lib.bgpo_grad_norm
+    assert norm(None, 2, 0, at(3), None, at(4), n, None) == INVALID
+    assert norm(g, -1, 0, at(3), None, at(4), n, None) == INVALID
+    for kind in (-1, 2):
+        assert norm(g, 2, kind, at(3), None, at(4), n, None) == INVALID
+    assert norm(g, 2, 0, None, None, at(4), n, None) == INVALID
+    assert norm(g, 2, 0, ctypes.c_void_p(at(3).value + 4), None, at(4), n, None) == INVALID
+    assert norm(g, 2, 0, at(3), ctypes.c_void_p(at(5).value + 2), at(4), n, None) == INVALID
+    assert norm(g, 2, 0, at(3), None, None, n, None) == WORKSPACE
+    assert norm(g, 2, 0, at(3), None, at(4), n - 1, None) == WORKSPACE
+    assert norm(g, 2, 0, at(3), None, ctypes.c_void_p(at(4).value + 4), n, None) == WORKSPACE
+    clip = b._lib.bgpo_grad_clip
+    for bad in (-1.0, math.nan, math.inf):
+        assert clip(g, None, 2, bad, at(3), None) == INVALID
+    assert clip(g, None, 2, 1.0, None, None) == INVALID
+    assert clip(g, None, 2, 1.0, ctypes.c_void_p(at(3).value + 4), None) == INVALID
+    assert clip(None, None, 0, 1.0, at(3), None) == 0                    # nothing to do
+    # outputs of another size, twice the same tensor, outputs over other entries
+    assert clip(g, _list(b, (1 << 47, 8, 1, 0), (1 << 48, 7, 0, 0)), 2, 1.0, at(3), None) == INVALID
+    a = 1 << 45
+    for entries in ([(a, 8, 1, 0), (a, 8, 1, 0)], [(a, 8, 1, 0), (a + 28, 8, 1, 0)], [(a + 28, 8, 0, 0), (a, 8, 1, 0)]):
+        assert clip(_list(b, *entries), None, 2, 1.0, at(3), None) == INVALID
+    two = _list(b, (a, 8, 1, 0), (a + 64, 8, 1, 0))
+    for outs in ([(a, 8, 0, 0), (1 << 47, 8, 1, 0)],                     # its own memory in another type
+                 [(a + 64, 8, 1, 0), (1 << 47, 8, 1, 0)], [(1 << 47, 8, 1, 0), (a + 60, 8, 1, 0)],
+                 [(1 << 47, 8, 1, 0), ((1 << 47) + 30, 8, 0, 0)]):
+        assert clip(two, _list(b, *outs), 2, 1.0, at(3), None) == INVALID
+
+
 def test_binding_refuses_tensors(b):
     cpu = torch.zeros(4, 8)
     i32, f32 = torch.zeros(4, dtype=torch.int32), torch.zeros(4)
@@ -241,3 +294,9 @@ def test_binding_refuses_tensors(b):
         b.bgpo_logits_logp(f32, i32, f32)
     with pytest.raises(ValueError, match="GPU"):
         b.bgpo_logits_logp_bwd(cpu, i32, f32, None, f32, None, cpu)
+    with pytest.raises(ValueError, match="GPU"):
+        b.GradList([cpu])
+    with pytest.raises(ValueError, match="GPU"):
+        b.bgpo_policy_loss(b.PolicyLoss(4, 8), cpu, None, None, f32, cpu, None, f32, None)
+    with pytest.raises(ValueError, match="GPU"):
+        b.bgpo_preference_loss(b.PreferenceLoss(4, 8), cpu, cpu, None, None, None, None, None, None, None, None, None, f32, None)
