@@ -124,7 +124,7 @@ typedef struct bgpo_policy {
   double clip_dual;   /* 0: none, or > 1 */
   double kl_coef;     /* finite */
   double loss_scale;  /* finite */
-  int32_t B, L;       /* responses, positions; B L <= 2^40 */
+  int32_t B, L;       /* responses, positions; L <= 2^30, B L <= 2^40 */
   int32_t dtype;      /* BGPO_F32 or BGPO_F64: logp, logp_old, logp_ref, dlogp */
   int32_t ratio, reduce, kl;
 } bgpo_policy;
@@ -183,7 +183,7 @@ typedef struct bgpo_preference {
   double margin;      /* finite */
   double label_smoothing;  /* 0 <= e < 1; 0 unless BGPO_PREF_SIGMOID */
   double loss_scale;  /* finite; 1/P: the mean over pairs */
-  int32_t P, L;       /* pairs, positions; P L <= 2^39 */
+  int32_t P, L;       /* pairs, positions; L <= 2^30, P L <= 2^39 */
   int32_t dtype;      /* BGPO_F32 or BGPO_F64: the [P, L] arrays */
   int32_t kind;       /* BGPO_PREF_* */
   int32_t mean;       /* 0: a response's score is the sum over its unmasked positions,

@@ -17,26 +17,301 @@
 namespace bgpo {
 
 constexpr int kThreads = 256;
-constexpr int kMaxWgs = 2048;       // workgroups of a pass, and rows of its partial sums
+constexpr int kStatsThreads = 512;
+constexpr int kMaxWgs = 4096;       // workgroups of a pass, and rows of its partial sums
 
-// Sum over the workgroup in a fixed order, returned to every thread; `red`
-// holds NV values per wave and is free again after the call's last barrier.
-template <int NV>
-__device__ __forceinline__ void wg_sum(double (&v)[NV], double (*red)[NV]) {
-  const int wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
+// Sum over groups of G lanes (G a power of two up to 64, or the workgroup), in
+// a fixed order, returned to every lane.  For a workgroup `red` holds NV values
+// per wave and is free again after the call.
+template <int G, int NV>
+__device__ __forceinline__ void group_sum(double (&v)[NV], double (*red)[NV]) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
+  for (int i = 0; i < NV; ++i)
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v[i] += __shfl_xor(v[i], off, 64);
-    if ((threadIdx.x & 63) == 0) red[wave][i] = v[i];
+    for (int off = (G < 64 ? G : 64) / 2; off > 0; off >>= 1) v[i] += __shfl_xor(v[i], off, 64);
+  if constexpr (G > 64) {
+    constexpr int kWaves = G / 64;
+    const int lane = threadIdx.x & 63;
+    if (lane == 0)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) red[threadIdx.x >> 6][i] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      v[i] = red[lane & (kWaves - 1)][i];
+#pragma unroll
+      for (int off = kWaves / 2; off > 0; off >>= 1) v[i] += __shfl_xor(v[i], off, 64);
+    }
+    __syncthreads();
+  }
+}
+
+// a b + c with the constant c as a scalar operand (as the addend in a vector
+// register it takes a move of its own each time)
+__device__ __forceinline__ double fma_const(double a, double b, double c) {
+  double r;
+  asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "s"(c));
+  return r;
+}
+
+// e^x and e^x - 1 in float64.  x = n ln2 + f with |f| <= ln2 / 2 (ln2 in two
+// parts, the first with enough zero bits that its product with n is exact) and
+// the series of e^f - 1 up to f^12 / 12!, whose remainder is below 2^-50.8 of f.
+// Half the instructions of the library functions, which bounded these kernels.
+// Past the range of doubles (infinities too) the value is put in at the end; a
+// NaN goes through.
+struct ExpParts {
+  double p;       // e^f - 1
+  int n;
+};
+__device__ __forceinline__ ExpParts exp_parts(double x) {
+  const double n = rint(x * 1.4426950408889634074);
+  double f = fma(n, -0x1.62e42fefa0000p-1, x);
+  f = fma(n, -0x1.cf79abc9e3b3ap-40, f);
+  double s = 1.0 / 479001600.0;
+  s = fma_const(s, f, 1.0 / 39916800.0);
+  s = fma_const(s, f, 1.0 / 3628800.0);
+  s = fma_const(s, f, 1.0 / 362880.0);
+  s = fma_const(s, f, 1.0 / 40320.0);
+  s = fma_const(s, f, 1.0 / 5040.0);
+  s = fma_const(s, f, 1.0 / 720.0);
+  s = fma_const(s, f, 1.0 / 120.0);
+  s = fma_const(s, f, 1.0 / 24.0);
+  s = fma_const(s, f, 1.0 / 6.0);
+  s = fma(s, f, 0.5);
+  return ExpParts{fma(s * f, f, f), (int)n};
+}
+__device__ __forceinline__ double exp64(double x) {
+  const ExpParts e = exp_parts(x);
+  const double y = ldexp(1.0 + e.p, e.n);
+  return x > 709.8 ? (double)INFINITY : x < -745.2 ? 0.0 : y;
+}
+// (1 + p in two parts, so that what the sum loses is kept where 2^n is near 1)
+__device__ __forceinline__ double expm1_64(double x) {
+  const ExpParts e = exp_parts(x);
+  const double h = 1.0 + e.p, l = (1.0 - h) + e.p;
+  const double y = (ldexp(h, e.n) - 1.0) + ldexp(l, e.n);
+  return x > 709.8 ? (double)INFINITY : x < -745.2 ? -1.0 : y;
+}
+
+// Number of this lane's group of G in its workgroup (a scalar where the lanes of
+// a wave share it, and with it the addresses of its rows).
+template <int G, int THREADS>
+__device__ __forceinline__ int group_index() {
+  if constexpr (G >= THREADS) return 0;
+  else if constexpr (G == 64) return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  else return (int)threadIdx.x / G;
+}
+// a value that a group shares, as a scalar where a wave does
+template <int G>
+__device__ __forceinline__ double scalar(double v) {
+  if constexpr (G < 64) {
+    return v;
+  } else {
+    const int2 w = __builtin_bit_cast(int2, v);
+    return __builtin_bit_cast(double, make_int2(__builtin_amdgcn_readfirstlane(w.x), __builtin_amdgcn_readfirstlane(w.y)));
+  }
+}
+
+// Four consecutive positions, and sixteen mask bytes, at any alignment of the
+// element type.
+typedef uint32_t raw16 __attribute__((ext_vector_type(4), aligned(4), may_alias));
+typedef uint32_t raw16b __attribute__((ext_vector_type(4), aligned(1), may_alias));
+typedef uint64_t raw16d __attribute__((ext_vector_type(2), aligned(8), may_alias));
+typedef uint32_t raw4 __attribute__((aligned(1), may_alias));
+
+__device__ __forceinline__ void load4(const float* p, float (&v)[4]) {
+  const raw16 r = *reinterpret_cast<const raw16*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void load4(const double* p, double (&v)[4]) {
+  const raw16d a = reinterpret_cast<const raw16d*>(p)[0], b = reinterpret_cast<const raw16d*>(p)[1];
+  v[0] = __longlong_as_double(a[0]);
+  v[1] = __longlong_as_double(a[1]);
+  v[2] = __longlong_as_double(b[0]);
+  v[3] = __longlong_as_double(b[1]);
+}
+__device__ __forceinline__ void store4(float* p, const float (&v)[4]) {
+  raw16 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(v[i]);
+  *reinterpret_cast<raw16*>(p) = r;
+}
+__device__ __forceinline__ void store4(double* p, const double (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    raw16d r;
+    r[0] = __double_as_longlong(v[2 * i]);
+    r[1] = __double_as_longlong(v[2 * i + 1]);
+    reinterpret_cast<raw16d*>(p)[i] = r;
+  }
+}
+
+// The positions that a lane of a short row takes at a time: U of them, G apart,
+// so that a group's accesses are contiguous whatever its alignment.  live[u]:
+// the position is before the end and counts.  Positions that do not count become
+// 0 in every array; they are not read unless another of the same wave's does.
+template <int G, int U>
+struct Positions {
+  bool live[U];
+  bool whole;         // every lane's positions are before the end
+
+  __device__ __forceinline__ void load(const uint8_t* mask, int i, int end) {
+    whole = !__any(i + (U - 1) * G >= end);
+    uint8_t m[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) m[u] = mask ? 0 : 1;
+    if (mask) {
+      if (whole) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) m[u] = mask[i + u * G];
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (i + u * G < end) m[u] = mask[i + u * G];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) live[u] = i + u * G < end && m[u] != 0;
+  }
+  __device__ __forceinline__ int count() const {
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) n += live[u] ? 1 : 0;
+    return n;
+  }
+  __device__ __forceinline__ bool any() const {
+    bool a = false;
+#pragma unroll
+    for (int u = 0; u < U; ++u) a = a || live[u];
+    return __any(a);
+  }
+  template <typename T>
+  __device__ __forceinline__ void values(const T* p, int i, T (&v)[U]) const {
+    if (whole) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = p[i + u * G];
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        v[u] = (T)0;
+        if (live[u]) v[u] = p[i + u * G];
+      }
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void select(T (&v)[U]) const {
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = live[u] ? v[u] : (T)0;
+  }
+  template <typename T>
+  __device__ __forceinline__ void store(T* p, int i, int end, const T (&v)[U]) const {
+    if (whole) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) p[i + u * G] = v[u];
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (i + u * G < end) p[i + u * G] = v[u];
+    }
+  }
+};
+
+// Long rows.  A row's mask is read first, 16 positions to a load: how many
+// count, and between which two all of them lie (a prompt before, padding after
+// them).  The arrays are then read only there, four positions to a lane, masked
+// ones too and without a condition: a load under a condition cannot be told from
+// one that was not made when a later one is waited for, so that nothing could be
+// in flight across a step.
+struct Range {
+  int n, first, last;       // positions that count; all of them lie in [first, last)
+};
+
+// of [i0, end), in every lane of the workgroup of G
+template <int G>
+__device__ __forceinline__ Range find_range(const uint8_t* mask, int i0, int end, int (*red)[3]) {
+  if (!mask) return Range{end - i0, i0, end};
+  int n = 0, first = end, last = i0;
+  auto word = [&](uint32_t w, int at) {
+    const uint32_t t = (((w & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w) & 0x80808080u;   // bytes that are not 0
+    if (!t) return;
+    n += __popc(t);
+    first = min(first, at + (__ffs((int)t) >> 3) - 1);
+    last = max(last, at + 4 - (__clz((int)t) >> 3));
+  };
+#pragma unroll 2
+  for (int j = i0 + (int)threadIdx.x * 16; j < end; j += G * 16) {
+    if (j + 16 <= end) {
+      const raw16b w = *reinterpret_cast<const raw16b*>(mask + j);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) word(w[k], j + 4 * k);
+    } else {
+      for (int k = j; k < end; ++k) word(mask[k], k);     // (one byte: a word with 0 above)
+    }
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    n += __shfl_xor(n, off, 64);
+    first = min(first, __shfl_xor(first, off, 64));
+    last = max(last, __shfl_xor(last, off, 64));
+  }
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) {
+    red[wave][0] = n;
+    red[wave][1] = first;
+    red[wave][2] = last;
   }
   __syncthreads();
+  n = 0;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    v[i] = 0.0;
-    for (int w = 0; w < n_waves; ++w) v[i] += red[w][i];
+  for (int w = 0; w < G / 64; ++w) {
+    n += red[w][0];
+    first = min(first, red[w][1]);
+    last = max(last, red[w][2]);
   }
   __syncthreads();
+  Range r{__builtin_amdgcn_readfirstlane(n), __builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(last)};
+  if (r.n == 0) r.last = r.first = end;
+  return r;
+}
+
+// The four positions of a lane at i: read at `at` = i, or before it where the row
+// (of L >= 4 positions) ends.
+struct Quad {
+  int i, at;
+  __device__ __forceinline__ Quad(int i, int L) : i(i), at(min(i, L - 4)) {}
+  __device__ __forceinline__ uint32_t mask(const uint8_t* m) const { return *reinterpret_cast<const raw4*>(m + at); }
+  // mask bytes of what lies in [i, last) alone
+  __device__ __forceinline__ uint32_t keep(uint32_t m, int last) const {
+    if (i + 4 <= last) return m;
+    const int before = i - at, after = at + 4 - last;
+    if (before > 3 || after > 3 || i >= last) return 0;
+    m = m >> (8 * before) << (8 * before);
+    return after > 0 ? m << (8 * after) >> (8 * after) : m;
+  }
+  template <typename T>
+  __device__ __forceinline__ void store(T* p, int last, const T (&v)[4]) const {
+    if (i + 4 <= last) {
+      store4(p + i, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (at + e >= i && at + e < last) p[at + e] = v[e];
+    }
+  }
+};
+__device__ __forceinline__ bool live(uint32_t m, int e) { return (m >> (8 * e) & 255) != 0; }
+
+// p[a .. b) = 0, by the workgroup of G
+template <int G, typename T>
+__device__ __forceinline__ void fill_zero(T* p, int a, int b) {
+  const T z[4] = {0, 0, 0, 0};
+  for (int i = a + (int)threadIdx.x * 4; i < b; i += G * 4) {
+    if (i + 4 <= b) store4(p + i, z);
+    else
+      for (int k = i; k < b; ++k) p[k] = 0;
+  }
 }
 
 // ---------------------------------------------------------------- policy loss
@@ -51,10 +326,15 @@ struct PolicyArgs {
   int64_t ld_logp, ld_old, ld_ref, ld_mask, ld_dlogp, ld_adv;
   int B, L, ratio, reduce, kl;
   double lo, hi, dual, kl_coef, loss_scale;
-  double2* rows;      // [B] unmasked positions and sum of d of each response
-  double* counts;     // [kMaxWgs] positions per workgroup of the first pass
+  // a response is taken in n_chunks pieces of `chunk` positions
+  int chunk, n_chunks;
+  double2* rows;      // [B n_chunks] unmasked positions and sum of d of each piece (NULL: no such pass)
+  double* counts;     // [kMaxWgs] positions per workgroup of that pass
   double* part;       // [kMaxWgs][kPolicySums]
-  int count_wgs;      // workgroups of the first pass (0: it did not run)
+  int count_wgs;      // its workgroups
+
+  __device__ uint32_t pieces() const { return (uint32_t)B * (uint32_t)n_chunks; }
+  __device__ bool whole_rows() const { return reduce == BGPO_REDUCE_RESPONSES || ratio == BGPO_RATIO_SEQUENCE; }
 };
 
 // objective, KL, log ratio, positions, cut positions
@@ -74,101 +354,364 @@ __device__ __forceinline__ Clipped clipped(double r, double A, const PolicyArgs&
   return c;
 }
 
-// the KL estimator and its derivative w.r.t. logp at q = ref - logp
-__device__ __forceinline__ void kl_term(int kind, double q, double* kl, double* dkl) {
-  if (kind == BGPO_KL_K1) {
-    *kl = -q;
-    *dkl = 1.0;
-  } else if (kind == BGPO_KL_K2) {
+// KL estimator of the instance: none, or BGPO_KL_* + 1
+enum { kNoKl = 0, kK1 = 1, kK2 = 2, kK3 = 3 };
+
+// the estimator and its derivative w.r.t. logp at q = ref - logp
+template <int KL>
+__device__ __forceinline__ void kl_term(double q, double* kl, double* dkl) {
+  if (KL == kK3) {
+    const double e = expm1_64(q);
+    *kl = e - q;
+    *dkl = -e;
+  } else if (KL == kK2) {
     *kl = 0.5 * q * q;
     *dkl = -q;
   } else {
-    const double e = expm1(q);
-    *kl = e - q;
-    *dkl = -e;
+    *kl = -q;
+    *dkl = 1.0;
   }
 }
 
-// First pass: unmasked positions and sum of d of each response, one workgroup
-// per response.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_policy_rows(PolicyArgs p) {
-  __shared__ double red[kThreads / 64][2];
-  double count = 0.0;
-  for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
-    double v[2] = {0.0, 0.0};
-    for (int i = threadIdx.x; i < p.L; i += kThreads)
-      if (p.mask[b * p.ld_mask + i]) {
-        v[0] += 1.0;
-        if (p.ratio == BGPO_RATIO_SEQUENCE && p.old)
-          v[1] += (double)static_cast<const T*>(p.logp)[b * p.ld_logp + i] -
-                  (double)static_cast<const T*>(p.old)[b * p.ld_old + i];
+// A response's unmasked positions and, for a sequence ratio, the sum of its d,
+// over [i0, end) (per lane; summed over the group by the caller).
+template <typename T, int G, bool TOKEN>
+__device__ __forceinline__ void row_terms(const PolicyArgs& p, int b, int i0, int end, double (&v)[2]) {
+  constexpr int U = 4;
+  const uint8_t* mask = p.mask + b * p.ld_mask;
+  const T* logp = static_cast<const T*>(p.logp) + b * p.ld_logp;
+  const T* old = static_cast<const T*>(p.old) + b * p.ld_old;
+  int n = 0;
+  double d = 0.0;
+  for (int j = i0; j < end; j += G * U) {
+    const int i = j + (int)(threadIdx.x % G);
+    Positions<G, U> k;
+    k.load(mask, i, end);
+    n += k.count();
+    if (!TOKEN && p.old && k.any()) {
+      T x[U], o[U];
+      k.values(logp, i, x);
+      k.values(old, i, o);
+#pragma unroll
+      for (int u = 0; u < U; ++u) d += k.live[u] ? (double)x[u] - (double)o[u] : 0.0;
+    }
+  }
+  v[0] = (double)n;
+  v[1] = d;
+}
+
+struct PolicySums {
+  double f = 0.0, kl = 0.0, d = 0.0;
+  int positions = 0, cuts = 0;
+};
+
+// What is the same for the whole response.
+struct PolicyRow {
+  double w, dkl_w, A;
+  double f, df;       // a sequence ratio's objective, and its gradient at every position
+  bool cut;
+};
+
+// the response's, from its positions n and its sum of d
+template <int G, bool TOKEN>
+__device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& p, int b, double w, double n, double d) {
+  if (p.reduce == BGPO_REDUCE_RESPONSES) w = n > 0.0 ? p.loss_scale / n : 0.0;
+  PolicyRow r{w, p.kl_coef * w, TOKEN && p.ld_adv ? 0.0 : (double)p.adv[b], 0.0, 0.0, false};
+  if (!TOKEN && n > 0.0) {
+    const double x = exp64(d / n);
+    const Clipped c = clipped(x, r.A, p);
+    r.f = c.f;
+    r.df = c.cut ? 0.0 : -w * x * r.A;      // n w / n
+    r.cut = c.cut;
+  }
+  r.w = scalar<G>(r.w);
+  r.dkl_w = scalar<G>(r.dkl_w);
+  r.A = scalar<G>(r.A);
+  r.f = scalar<G>(r.f);
+  r.df = scalar<G>(r.df);
+  return r;
+}
+
+// Objective and gradient of one position.  (A masked one counts as 0 everywhere:
+// r = 1, A = 0, q = 0.)
+template <bool TOKEN, int KL, typename T>
+__device__ __forceinline__ T position_loss(const PolicyArgs& p, const PolicyRow& row, bool live, T x, T o, T q, double A,
+                                           PolicySums& s, T& bad) {
+  double ge = row.df;
+  if (TOKEN) {
+    const double d = p.old && live ? (double)x - (double)o : 0.0;
+    const Clipped c = clipped(exp64(d), live ? A : 0.0, p);
+    ge = c.cut ? 0.0 : -row.w * c.f;        // (f = r A where the clip does not hold it)
+    s.f += c.f;
+    s.d += d;
+    s.cuts += c.cut ? 1 : 0;
+  }
+  if (KL) {
+    double kl, dkl;
+    kl_term<KL>(live ? (double)q - (double)x : 0.0, &kl, &dkl);
+    s.kl += kl;
+    if (p.kl_coef != 0.0) ge = fma(row.dkl_w, dkl, ge);
+  }
+  const T g = live ? (T)ge : (T)0;
+  bad = fma(g, (T)0, bad);                  // (NaN once one is not finite)
+  return g;
+}
+
+// Objective and gradient of [i0, end) of a response.
+template <typename T, int G, bool TOKEN, int KL>
+__device__ __forceinline__ void row_loss(const PolicyArgs& p, const PolicyRow& row, int b, int i0, int end, PolicySums& s,
+                                         T& bad) {
+  constexpr int U = 4;
+  const uint8_t* mask = p.mask + b * p.ld_mask;
+  const T* logp = static_cast<const T*>(p.logp) + b * p.ld_logp;
+  const T* old = static_cast<const T*>(p.old) + b * p.ld_old;
+  const T* ref = static_cast<const T*>(p.ref) + b * p.ld_ref;
+  const float* adv = p.adv + b * p.ld_adv;
+  T* dlogp = static_cast<T*>(p.dlogp) + b * p.ld_dlogp;
+  for (int j = i0; j < end; j += G * U) {
+    const int i = j + (int)(threadIdx.x % G);
+    Positions<G, U> k;
+    k.load(mask, i, end);
+    T g[U] = {0, 0, 0, 0};
+    if (k.any()) {
+      T x[U] = {0, 0, 0, 0}, o[U] = {0, 0, 0, 0}, q[U] = {0, 0, 0, 0};
+      float A[U];
+      if (TOKEN || KL) k.values(logp, i, x);
+      if (TOKEN && p.old) k.values(old, i, o);
+      if (KL) k.values(ref, i, q);
+      if (TOKEN && p.ld_adv) k.values(adv, i, A);
+      s.positions += k.count();
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        g[u] = position_loss<TOKEN, KL>(p, row, k.live[u], x[u], o[u], q[u], p.ld_adv ? (double)A[u] : row.A, s, bad);
+        if (u % 2) __builtin_amdgcn_sched_barrier(0);   // (two exponentials at a time: more take registers)
       }
-    wg_sum<2>(v, red);
-    if (threadIdx.x == 0) p.rows[b] = make_double2(v[0], v[1]);
+    }
+    if (p.dlogp) k.store(dlogp, i, end, g);
+  }
+}
+
+template <bool TOKEN>
+__device__ __forceinline__ void add_sums(const PolicyRow& row, const PolicySums& s, double (&sums)[kPolicySums]) {
+  sums[0] -= row.w * (TOKEN ? s.f : s.positions * row.f);
+  sums[1] += row.w * s.kl;
+  sums[2] += row.w * s.d;
+  sums[3] += (double)s.positions;
+  sums[4] += (double)(TOKEN ? s.cuts : row.cut ? s.positions : 0);
+}
+
+// First pass: the terms of every piece, to p.rows; returns the positions that
+// the lane's group has seen.
+template <typename T, int G, bool TOKEN>
+__device__ __forceinline__ double rows_pass(const PolicyArgs& p, int group, int n_groups, double (*red)[2]) {
+  double count = 0.0;
+  for (uint32_t k = group; k < p.pieces(); k += n_groups) {
+    const int b = (int)(k / (uint32_t)p.n_chunks), i0 = (int)(k % (uint32_t)p.n_chunks) * p.chunk;
+    double v[2];
+    row_terms<T, G, TOKEN>(p, b, i0, min(p.L, i0 + p.chunk), v);
+    group_sum<G, 2>(v, red);
+    if (threadIdx.x % G == 0) p.rows[k] = make_double2(v[0], v[1]);
     count += v[0];
   }
-  if (threadIdx.x == 0) p.counts[blockIdx.x] = count;
+  return count;
 }
 
-// Second pass: loss and gradient, one workgroup per response.
-template <typename T>
+// Second pass: the loss and the gradient of every piece.  `w` is the weight of
+// a position where it is the same everywhere.
+template <typename T, int G, bool TOKEN, int KL>
+__device__ __forceinline__ void loss_pass(const PolicyArgs& p, int group, int n_groups, double w,
+                                          double (&sums)[kPolicySums], T& bad, double (*red)[2]) {
+  const int lane = threadIdx.x % G;
+  for (uint32_t k = group; k < p.pieces(); k += n_groups) {
+    const int b = (int)(k / (uint32_t)p.n_chunks), i0 = (int)(k % (uint32_t)p.n_chunks) * p.chunk;
+    const int end = min(p.L, i0 + p.chunk);
+    double v[2] = {0.0, 0.0};             // positions and sum of d of the response
+    if (p.whole_rows()) {
+      if (p.rows) {
+        for (int c = lane; c < p.n_chunks; c += G) {
+          const double2 r = p.rows[(int64_t)b * p.n_chunks + c];
+          v[0] += r.x;
+          v[1] += r.y;
+        }
+      } else {
+        row_terms<T, G, TOKEN>(p, b, i0, end, v);
+      }
+      group_sum<G, 2>(v, red);
+    }
+    const PolicyRow row = policy_row<G, TOKEN>(p, b, w, v[0], v[1]);
+    PolicySums s;
+    if (!TOKEN && lane == 0 && i0 == 0) s.d = v[1];
+    row_loss<T, G, TOKEN, KL>(p, row, b, i0, end, s, bad);
+    add_sums<TOKEN>(row, s, sums);
+  }
+}
+
+// The same passes over long rows, a piece to a workgroup.
+
+// the sum of d over a piece's range, per lane
+template <typename T, int G>
+__device__ __forceinline__ double range_log_ratio(const PolicyArgs& p, int b, const Range& r) {
+  const uint8_t* mask = p.mask + b * p.ld_mask;
+  const T* logp = static_cast<const T*>(p.logp) + b * p.ld_logp;
+  const T* old = static_cast<const T*>(p.old) + b * p.ld_old;
+  double d = 0.0;
+  constexpr int U = 2;
+  for (int j = r.first + (int)threadIdx.x * 4; j < r.last; j += G * 4 * U) {
+    T x[U][4], o[U][4];
+    uint32_t m[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const Quad k(j + u * G * 4, p.L);
+      m[u] = k.mask(mask);
+      load4(logp + k.at, x[u]);
+      load4(old + k.at, o[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      m[u] = Quad(j + u * G * 4, p.L).keep(m[u], r.last);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) d += live(m[u], e) ? (double)x[u][e] - (double)o[u][e] : 0.0;
+    }
+  }
+  return d;
+}
+
+template <typename T, int G, bool TOKEN>
+__device__ __forceinline__ double long_rows_pass(const PolicyArgs& p, int (*ired)[3], double (*red)[2]) {
+  double count = 0.0;
+  for (uint32_t k = blockIdx.x; k < p.pieces(); k += gridDim.x) {
+    const int b = (int)(k / (uint32_t)p.n_chunks), i0 = (int)(k % (uint32_t)p.n_chunks) * p.chunk;
+    const Range r = find_range<G>(p.mask + b * p.ld_mask, i0, min(p.L, i0 + p.chunk), ired);
+    double v[1] = {0.0};
+    if (!TOKEN && p.old && r.n) {
+      v[0] = range_log_ratio<T, G>(p, b, r);
+      group_sum<G, 1>(v, reinterpret_cast<double(*)[1]>(red));
+    }
+    if (threadIdx.x == 0) p.rows[k] = make_double2((double)r.n, v[0]);
+    count += (double)r.n;
+  }
+  return count;
+}
+
+template <typename T, int G, bool TOKEN, int KL, bool ADV>
+__device__ __forceinline__ void long_loss_pass(const PolicyArgs& p, double w, double (&sums)[kPolicySums], T& bad,
+                                               int (*ired)[3], double (*red)[2]) {
+  struct Tile {
+    uint32_t m;
+    T x[4], o[4], q[4];
+    float A[4];
+  };
+  for (uint32_t piece = blockIdx.x; piece < p.pieces(); piece += gridDim.x) {
+    const int b = (int)(piece / (uint32_t)p.n_chunks), i0 = (int)(piece % (uint32_t)p.n_chunks) * p.chunk;
+    const int end = min(p.L, i0 + p.chunk);
+    const uint8_t* mask = p.mask + b * p.ld_mask;
+    const T* logp = static_cast<const T*>(p.logp) + b * p.ld_logp;
+    // (on-policy d is 0, whatever is read in its place)
+    const T* old = p.old ? static_cast<const T*>(p.old) + b * p.ld_old : logp;
+    const T* ref = static_cast<const T*>(p.ref) + b * p.ld_ref;
+    const float* adv = p.adv + b * p.ld_adv;
+    T* dlogp = static_cast<T*>(p.dlogp) + b * p.ld_dlogp;
+    const Range r = find_range<G>(mask, i0, end, ired);
+    double v[2] = {(double)r.n, 0.0};     // positions and sum of d of the response
+    if (p.whole_rows()) {
+      if (p.rows) {
+        v[0] = 0.0;
+        for (int c = threadIdx.x; c < p.n_chunks; c += G) {
+          const double2 t = p.rows[(int64_t)b * p.n_chunks + c];
+          v[0] += t.x;
+          v[1] += t.y;
+        }
+        group_sum<G, 2>(v, red);
+      } else if (!TOKEN && p.old && r.n) {
+        double d[1] = {range_log_ratio<T, G>(p, b, r)};
+        group_sum<G, 1>(d, reinterpret_cast<double(*)[1]>(red));
+        v[1] = d[0];
+      }
+    }
+    const PolicyRow row = policy_row<G, TOKEN>(p, b, w, v[0], v[1]);
+    PolicySums s;
+    if (!TOKEN && threadIdx.x == 0 && i0 == 0) s.d = v[1];
+    if (p.dlogp) {
+      fill_zero<G>(dlogp, i0, r.first);
+      fill_zero<G>(dlogp, r.last, end);
+    }
+    // a step's loads are issued before the step before it is computed and stored
+    auto load = [&](Tile& t, int i) {
+      const Quad k(i, p.L);
+      t.m = k.mask(mask);
+      if (TOKEN || KL) load4(logp + k.at, t.x);
+      if (TOKEN) load4(old + k.at, t.o);
+      if (KL) load4(ref + k.at, t.q);
+      if (ADV) load4(adv + k.at, t.A);
+    };
+    auto step = [&](const Tile& t, int i) {
+      const Quad k(i, p.L);
+      const uint32_t m = k.keep(t.m, r.last);
+      T g[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s.positions += live(m, e) ? 1 : 0;
+        g[e] = position_loss<TOKEN, KL>(p, row, live(m, e), t.x[e], t.o[e], t.q[e], ADV ? (double)t.A[e] : row.A, s, bad);
+        if (e % 2) __builtin_amdgcn_sched_barrier(0);   // (two exponentials at a time: more take registers)
+      }
+      if (p.dlogp) k.store(dlogp, r.last, g);
+    };
+    if (r.n) {
+      Tile t, next;
+      load(t, r.first + (int)threadIdx.x * 4);
+      for (int j = r.first; j < r.last; j += G * 4) {
+        const int i = j + (int)threadIdx.x * 4;
+        load(next, i + G * 4);
+        step(t, i);
+        t = next;
+      }
+    }
+    add_sums<TOKEN>(row, s, sums);
+  }
+}
+
+template <typename T, int G, bool TOKEN>
+__global__ __launch_bounds__(kThreads) void k_policy_rows(PolicyArgs p) {
+  constexpr int kWg = kThreads, kGroups = kWg / G;
+  __shared__ double red[kWg / 64][2];
+  double v[1];
+  if constexpr (G > 64) {
+    __shared__ int ired[kWg / 64][3];
+    v[0] = long_rows_pass<T, G, TOKEN>(p, ired, red);
+  } else {
+    v[0] = rows_pass<T, G, TOKEN>(p, blockIdx.x * kGroups + group_index<G, kWg>(), gridDim.x * kGroups, red);
+  }
+  if (threadIdx.x % G) v[0] = 0.0;
+  group_sum<kWg, 1>(v, reinterpret_cast<double(*)[1]>(red));
+  if (threadIdx.x == 0) p.counts[blockIdx.x] = v[0];
+}
+
+template <typename T, int G, bool TOKEN, int KL>
 __global__ __launch_bounds__(kThreads) void k_policy_loss(PolicyArgs p) {
-  __shared__ double red[kThreads / 64][kPolicySums];
-  double sums[kPolicySums] = {0.0, 0.0, 0.0, 0.0, 0.0};
+  constexpr int kWg = kThreads, kGroups = kWg / G;
+  __shared__ double red[kWg / 64][kPolicySums];
   double w = p.loss_scale;
   if (p.reduce == BGPO_REDUCE_TOKENS) {
     double n[1] = {0.0};
-    for (int i = threadIdx.x; i < p.count_wgs; i += kThreads) n[0] += p.counts[i];
-    wg_sum<1>(n, reinterpret_cast<double(*)[1]>(red));
+    for (int i = threadIdx.x; i < p.count_wgs; i += kWg) n[0] += p.counts[i];
+    group_sum<kWg, 1>(n, reinterpret_cast<double(*)[1]>(red));
     w = n[0] > 0.0 ? p.loss_scale / n[0] : 0.0;
   }
-  bool bad = false;
-  for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
-    const double n = p.count_wgs ? p.rows[b].x : 1.0;
-    if (p.reduce == BGPO_REDUCE_RESPONSES) w = n > 0.0 ? p.loss_scale / n : 0.0;
-    // one ratio for the response: its objective at every position, and the
-    // gradient of its n weights by d of one position
-    Clipped row{0.0, false};
-    double drow = 0.0;
-    if (p.ratio == BGPO_RATIO_SEQUENCE && n > 0.0) {
-      const double A = p.adv[b], r = exp(p.rows[b].y / n);
-      row = clipped(r, A, p);
-      drow = row.cut ? 0.0 : -w * r * A;      // n w / n
-    }
-    for (int i = threadIdx.x; i < p.L; i += kThreads) {
-      double g = 0.0;
-      if (p.mask[b * p.ld_mask + i]) {
-        const double lp = static_cast<const T*>(p.logp)[b * p.ld_logp + i];
-        const double d = p.old ? lp - (double)static_cast<const T*>(p.old)[b * p.ld_old + i] : 0.0;
-        Clipped c = row;
-        g = drow;
-        if (p.ratio == BGPO_RATIO_TOKEN) {
-          const double A = p.ld_adv ? p.adv[b * p.ld_adv + i] : p.adv[b], r = exp(d);
-          c = clipped(r, A, p);
-          g = c.cut ? 0.0 : -w * r * A;
-        }
-        if (p.ref) {
-          double kl, dkl;
-          kl_term(p.kl, (double)static_cast<const T*>(p.ref)[b * p.ld_ref + i] - lp, &kl, &dkl);
-          sums[1] += w * kl;
-          if (p.kl_coef != 0.0) g += p.kl_coef * w * dkl;
-        }
-        sums[0] -= w * c.f;
-        sums[2] += w * d;
-        sums[3] += 1.0;
-        sums[4] += c.cut ? 1.0 : 0.0;
-      }
-      if (p.dlogp) {
-        const T o = (T)g;
-        bad = bad || !isfinite(o);
-        static_cast<T*>(p.dlogp)[b * p.ld_dlogp + i] = o;
-      }
-    }
+  double sums[kPolicySums] = {0.0, 0.0, 0.0, 0.0, 0.0};
+  T bad = 0;
+  double(*red2)[2] = reinterpret_cast<double(*)[2]>(red);
+  if constexpr (G > 64) {
+    __shared__ int ired[kWg / 64][3];
+    if (TOKEN && p.ld_adv) long_loss_pass<T, G, TOKEN, KL, TOKEN>(p, w, sums, bad, ired, red2);
+    else long_loss_pass<T, G, TOKEN, KL, false>(p, w, sums, bad, ired, red2);
+  } else {
+    loss_pass<T, G, TOKEN, KL>(p, blockIdx.x * kGroups + group_index<G, kWg>(), gridDim.x * kGroups, w, sums, bad, red2);
   }
-  if (bad && p.flags) atomicOr(p.flags, kFlagNonfinite);
-  wg_sum<kPolicySums>(sums, red);
-  if (threadIdx.x < kPolicySums) p.part[blockIdx.x * kPolicySums + threadIdx.x] = sums[threadIdx.x];
+  if (bad != bad && p.dlogp && p.flags) atomicOr(p.flags, kFlagNonfinite);
+  group_sum<kWg, kPolicySums>(sums, red);
+  if (threadIdx.x == 0)
+#pragma unroll
+    for (int i = 0; i < kPolicySums; ++i) p.part[blockIdx.x * kPolicySums + i] = sums[i];
 }
 
 __device__ void write_policy_stats(const PolicyArgs& p, const double (&s)[kPolicySums]) {
@@ -182,14 +725,39 @@ __device__ void write_policy_stats(const PolicyArgs& p, const double (&s)[kPolic
   if (!isfinite(loss) && p.flags) atomicOr(p.flags, kFlagNonfinite);
 }
 
-__global__ __launch_bounds__(kThreads) void k_policy_stats(PolicyArgs p, int wgs) {
-  __shared__ double red[kThreads / 64][kPolicySums];
+__global__ __launch_bounds__(kStatsThreads) void k_policy_stats(PolicyArgs p, int wgs) {
+  __shared__ double red[kStatsThreads / 64][kPolicySums];
   double s[kPolicySums] = {0.0, 0.0, 0.0, 0.0, 0.0};
-  for (int i = threadIdx.x; i < wgs; i += kThreads)
+#pragma unroll 4
+  for (int i = threadIdx.x; i < wgs; i += kStatsThreads)
 #pragma unroll
     for (int c = 0; c < kPolicySums; ++c) s[c] += p.part[i * kPolicySums + c];
-  wg_sum<kPolicySums>(s, red);
+  group_sum<kStatsThreads, kPolicySums>(s, red);
   if (threadIdx.x == 0) write_policy_stats(p, s);
+}
+
+// A small batch in one launch of one workgroup: the passes above with barriers
+// between them, pieces of four positions to a lane.
+constexpr int kSmallThreads = 1024;
+
+template <typename T, int G, bool TOKEN, int KL>
+__global__ __launch_bounds__(kSmallThreads) void k_policy_small(PolicyArgs p) {
+  constexpr int kGroups = kSmallThreads / G;
+  __shared__ double red[kSmallThreads / 64][kPolicySums];
+  const int group = group_index<G, kSmallThreads>();
+  double w = p.loss_scale;
+  if (p.rows) {
+    double n[1] = {rows_pass<T, G, TOKEN>(p, group, kGroups, nullptr)};
+    if (threadIdx.x % G) n[0] = 0.0;
+    group_sum<kSmallThreads, 1>(n, reinterpret_cast<double(*)[1]>(red));   // (its barriers publish p.rows)
+    if (p.reduce == BGPO_REDUCE_TOKENS) w = n[0] > 0.0 ? p.loss_scale / n[0] : 0.0;
+  }
+  double sums[kPolicySums] = {0.0, 0.0, 0.0, 0.0, 0.0};
+  T bad = 0;
+  loss_pass<T, G, TOKEN, KL>(p, group, kGroups, w, sums, bad, nullptr);
+  if (bad != bad && p.dlogp && p.flags) atomicOr(p.flags, kFlagNonfinite);
+  group_sum<kSmallThreads, kPolicySums>(sums, red);
+  if (threadIdx.x == 0) write_policy_stats(p, sums);
 }
 
 static int check_policy(const bgpo_policy* p) {
@@ -201,26 +769,87 @@ static int check_policy(const bgpo_policy* p) {
       !isfinite(p->kl_coef) || !isfinite(p->loss_scale) || p->ld_adv < 0 ||
       (p->ld_adv && p->ratio != BGPO_RATIO_TOKEN))
     return BGPO_ERR_INVALID_ARG;
-  if ((int64_t)p->B * p->L > int64_t(1) << 40) return BGPO_ERR_UNSUPPORTED;
+  if (p->L > 1 << 30 || (int64_t)p->B * p->L > int64_t(1) << 40) return BGPO_ERR_UNSUPPORTED;
   return BGPO_OK;
 }
 
-static size_t policy_bytes(const bgpo_policy* p) {
-  return (size_t)p->B * sizeof(double2) + kMaxWgs * (kPolicySums + 1) * sizeof(double);
+// How the responses are cut into pieces, and the lanes that take one.
+struct PolicyPlan {
+  bool small, rows_pass;
+  int lanes, chunk, n_chunks;
+  int64_t pieces;
+};
+
+// Up to this many positions are one workgroup's work: one launch instead of two
+// or three.
+constexpr int64_t kSmallBatch = 8192;
+
+// Pieces of rows of L positions.
+static void cut_rows(int64_t rows, int64_t L, PolicyPlan* q) {
+  q->small = rows * L <= kSmallBatch;
+  int64_t n = 1;
+  if (q->small) {
+    q->lanes = L <= 64 ? 16 : 64;
+    n = rows < kSmallThreads / q->lanes ? (L + q->lanes * 4 - 1) / (q->lanes * 4) : 1;
+  } else {
+    q->lanes = L <= 64 ? 16 : L <= 512 ? 64 : kThreads;
+    n = std::max<int64_t>(1, std::min<int64_t>((512 + rows - 1) / rows, L / 4096));
+  }
+  q->chunk = (int)((L + n - 1) / n);
+  q->n_chunks = (int)((L + q->chunk - 1) / q->chunk);
+  q->pieces = rows * q->n_chunks;
 }
 
-template <typename T>
-static int run_policy(PolicyArgs p, hipStream_t s) {
-  const unsigned wgs = (unsigned)std::min<int64_t>(p.B, kMaxWgs);
-  if (p.reduce != BGPO_REDUCE_SUM || p.ratio == BGPO_RATIO_SEQUENCE) {
+static PolicyPlan plan_policy(const bgpo_policy* p) {
+  PolicyPlan q;
+  cut_rows(p->B, p->L, &q);
+  const bool whole = p->reduce == BGPO_REDUCE_RESPONSES || p->ratio == BGPO_RATIO_SEQUENCE;
+  q.rows_pass = p->reduce == BGPO_REDUCE_TOKENS || (whole && q.n_chunks > 1);
+  return q;
+}
+
+static size_t policy_bytes(const PolicyPlan& q) {
+  return (q.rows_pass ? (size_t)q.pieces * sizeof(double2) : 0) +
+         (q.small ? 0 : kMaxWgs * (kPolicySums + 1) * sizeof(double)) + 256;
+}
+
+template <typename T, int G, bool TOKEN, int KL>
+static int launch_policy(PolicyArgs p, const PolicyPlan& q, hipStream_t s) {
+  constexpr int kWg = kThreads, kGroups = kWg / G;
+  const unsigned wgs = (unsigned)std::min<int64_t>((q.pieces + kGroups - 1) / kGroups, kMaxWgs);
+  if (q.rows_pass) {
     p.count_wgs = (int)wgs;
-    k_policy_rows<T><<<wgs, kThreads, 0, s>>>(p);
+    k_policy_rows<T, G, TOKEN><<<wgs, kWg, 0, s>>>(p);
     if (hipGetLastError() != hipSuccess) return BGPO_ERR_HIP;
   }
-  k_policy_loss<T><<<wgs, kThreads, 0, s>>>(p);
+  k_policy_loss<T, G, TOKEN, KL><<<wgs, kWg, 0, s>>>(p);
   if (hipGetLastError() != hipSuccess) return BGPO_ERR_HIP;
-  k_policy_stats<<<1, kThreads, 0, s>>>(p, (int)wgs);
+  k_policy_stats<<<1, kStatsThreads, 0, s>>>(p, (int)wgs);
   return hipGetLastError() == hipSuccess ? BGPO_OK : BGPO_ERR_HIP;
+}
+
+template <typename T, bool TOKEN, int KL>
+static int run_policy(const PolicyArgs& p, const PolicyPlan& q, hipStream_t s) {
+  if (q.small) {
+    if (q.lanes == 16) k_policy_small<T, 16, TOKEN, KL><<<1, kSmallThreads, 0, s>>>(p);
+    else k_policy_small<T, 64, TOKEN, KL><<<1, kSmallThreads, 0, s>>>(p);
+    return hipGetLastError() == hipSuccess ? BGPO_OK : BGPO_ERR_HIP;
+  }
+  switch (q.lanes) {
+    case 16: return launch_policy<T, 16, TOKEN, KL>(p, q, s);
+    case 64: return launch_policy<T, 64, TOKEN, KL>(p, q, s);
+    default: return launch_policy<T, kThreads, TOKEN, KL>(p, q, s);
+  }
+}
+
+template <typename T, bool TOKEN>
+static int run_policy(const PolicyArgs& p, const PolicyPlan& q, hipStream_t s) {
+  switch (!p.ref ? kNoKl : p.kl + 1) {
+    case kNoKl: return run_policy<T, TOKEN, kNoKl>(p, q, s);
+    case kK1: return run_policy<T, TOKEN, kK1>(p, q, s);
+    case kK2: return run_policy<T, TOKEN, kK2>(p, q, s);
+    default: return run_policy<T, TOKEN, kK3>(p, q, s);
+  }
 }
 
 // ---------------------------------------------------------------- preference loss
@@ -242,9 +871,16 @@ struct PrefArgs {
   int64_t adv_stride;
   int P, L, kind, mean;
   double beta, margin, smoothing, loss_scale;
-  double2* part;      // [kMaxWgs] loss and count of m > 0
-  double* msum;       // [kMaxWgs] sum of m
+  // a pair is taken in n_chunks pieces of `chunk` positions of either response
+  int chunk, n_chunks;
+  double* scores;     // [P n_chunks][4] sum and positions of either side (NULL: no such pass)
+  double* part;       // [kMaxWgs][kPrefSums]
+
+  __device__ uint32_t pieces() const { return (uint32_t)P * (uint32_t)n_chunks; }
 };
+
+// loss, pairs with m > 0, sum of m
+constexpr int kPrefSums = BGPO_PREF_STATS;
 
 // log(1 + e^v) without overflow
 __device__ __forceinline__ double softplus(double v) { return fmax(v, 0.0) + log1p(exp(-fabs(v))); }
@@ -265,71 +901,246 @@ __device__ __forceinline__ void pref_term(const PrefArgs& p, double m, double* l
   }
 }
 
-// One workgroup per pair: the scores of both responses, the margin's loss, and
-// the gradient, which is one number per response.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_preference(PrefArgs p) {
-  __shared__ double red[kThreads / 64][4];
-  double loss_sum = 0.0, right = 0.0, m_sum = 0.0;
-  bool bad = false;
-  for (int q = blockIdx.x; q < p.P; q += gridDim.x) {
-    double v[4] = {0.0, 0.0, 0.0, 0.0};     // score and positions of either side
+// Sum and unmasked positions of a piece of both responses (per lane).
+template <typename T, int G>
+__device__ __forceinline__ void pair_terms(const PrefArgs& p, int q, int i0, int end, double (&v)[4]) {
+  constexpr int U = 4;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const PrefSide& s = p.side[k];
-      for (int i = threadIdx.x; i < p.L; i += kThreads)
-        if (!s.mask || s.mask[q * s.ld_mask + i]) {
-          double x = static_cast<const T*>(s.theta)[q * s.ld + i];
-          if (s.ref) x -= (double)static_cast<const T*>(s.ref)[q * s.ld_ref + i];
-          v[2 * k] += x;
-          v[2 * k + 1] += 1.0;
-        }
+  for (int c = 0; c < 2; ++c) {
+    const PrefSide& s = p.side[c];
+    const uint8_t* mask = s.mask ? s.mask + q * s.ld_mask : nullptr;
+    const T* theta = static_cast<const T*>(s.theta) + q * s.ld;
+    const T* ref = static_cast<const T*>(s.ref) + q * s.ld_ref;
+    double sum = 0.0;
+    int n = 0;
+    for (int j = i0; j < end; j += U * G) {
+      const int i = j + (int)(threadIdx.x % G);
+      Positions<G, U> k;
+      k.load(mask, i, end);
+      n += k.count();
+      if (!k.any()) continue;
+      T x[U], r[U];
+      k.values(theta, i, x);
+      if (s.ref) k.values(ref, i, r);
+#pragma unroll
+      for (int u = 0; u < U; ++u) sum += !k.live[u] ? 0.0 : s.ref ? (double)x[u] - (double)r[u] : (double)x[u];
     }
-    wg_sum<4>(v, red);
+    v[2 * c] = sum;
+    v[2 * c + 1] = (double)n;
+  }
+}
+
+// The sum over a long row's range.
+template <typename T, int G, bool MASK, bool REF>
+__device__ __forceinline__ double range_score(const PrefArgs& p, const PrefSide& s, int q, const Range& r) {
+  const uint8_t* mask = s.mask + q * s.ld_mask;
+  const T* theta = static_cast<const T*>(s.theta) + q * s.ld;
+  const T* ref = static_cast<const T*>(s.ref) + q * s.ld_ref;
+  double sum = 0.0;
+  constexpr int U = 4;
+  for (int j = r.first + (int)threadIdx.x * 4; j < r.last; j += G * 4 * U) {
+    T x[U][4], o[U][4];
+    uint32_t m[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const Quad k(j + u * G * 4, p.L);
+      m[u] = MASK ? k.mask(mask) : 0x01010101u;
+      load4(theta + k.at, x[u]);
+      if (REF) load4(ref + k.at, o[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      m[u] = Quad(j + u * G * 4, p.L).keep(m[u], r.last);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += !live(m[u], e) ? 0.0 : REF ? (double)x[u][e] - (double)o[u][e] : (double)x[u][e];
+    }
+  }
+  return sum;
+}
+
+// Sum and unmasked positions of a long row's piece of both responses, in every
+// lane of the workgroup, and their ranges.
+template <typename T, int G>
+__device__ __forceinline__ void long_pair_terms(const PrefArgs& p, int q, int i0, int end, Range (&range)[2], double (&v)[4],
+                                                double (*red)[2], int (*ired)[3]) {
+  double d[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const PrefSide& s = p.side[c];
+    range[c] = find_range<G>(s.mask ? s.mask + q * s.ld_mask : nullptr, i0, end, ired);
+  }
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const PrefSide& s = p.side[c];
+    d[c] = s.mask ? s.ref ? range_score<T, G, true, true>(p, s, q, range[c]) : range_score<T, G, true, false>(p, s, q, range[c])
+                  : s.ref ? range_score<T, G, false, true>(p, s, q, range[c]) : range_score<T, G, false, false>(p, s, q, range[c]);
+  }
+  group_sum<G, 2>(d, red);
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    v[2 * c] = d[c];
+    v[2 * c + 1] = (double)range[c].n;
+  }
+}
+
+// g at the positions of a long row's range that count, 0 at the others of the
+// piece.
+template <typename T, int G>
+__device__ __forceinline__ void range_gradient(const PrefArgs& p, const PrefSide& s, int q, int i0, int end, const Range& r, T g) {
+  T* grad = static_cast<T*>(s.grad) + q * s.ld_grad;
+  fill_zero<G>(grad, i0, r.first);
+  fill_zero<G>(grad, r.last, end);
+  const uint8_t* mask = s.mask + q * s.ld_mask;
+  for (int j = r.first + (int)threadIdx.x * 4; j < r.last; j += G * 4) {
+    const Quad k(j, p.L);
+    const uint32_t m = r.n == r.last - r.first ? 0x01010101u : k.mask(mask);
+    T o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = live(m, e) ? g : (T)0;
+    k.store(grad, r.last, o);
+  }
+}
+
+// First pass: these terms of every piece.
+template <typename T, int G>
+__device__ __forceinline__ void scores_pass(const PrefArgs& p, int group, int n_groups, double (*red)[2], int (*ired)[3]) {
+  for (uint32_t k = group; k < p.pieces(); k += n_groups) {
+    const int q = (int)(k / (uint32_t)p.n_chunks), i0 = (int)(k % (uint32_t)p.n_chunks) * p.chunk;
+    const int end = min(p.L, i0 + p.chunk);
+    double v[4];
+    if constexpr (G > 64) {
+      Range r[2];
+      long_pair_terms<T, G>(p, q, i0, end, r, v, red, ired);
+    } else {
+      pair_terms<T, G>(p, q, i0, end, v);
+      group_sum<G, 4>(v, nullptr);
+    }
+    if (threadIdx.x % G == 0)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) p.scores[(int64_t)k * 4 + c] = v[c];
+  }
+}
+
+// Second pass: the margin's loss, and the gradient, which is one number per
+// response.
+template <typename T, int G>
+__device__ __forceinline__ void pairs_pass(const PrefArgs& p, int group, int n_groups, double (&sums)[kPrefSums],
+                                           bool& bad, double (*red)[4], int (*ired)[3]) {
+  const int lane = threadIdx.x % G;
+  for (uint32_t k = group; k < p.pieces(); k += n_groups) {
+    const int q = (int)(k / (uint32_t)p.n_chunks), i0 = (int)(k % (uint32_t)p.n_chunks) * p.chunk;
+    const int end = min(p.L, i0 + p.chunk);
+    double v[4] = {0.0, 0.0, 0.0, 0.0};
+    Range range[2];
+    if (p.scores) {
+      if constexpr (G > 64)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          range[c] = find_range<G>(p.side[c].mask ? p.side[c].mask + q * p.side[c].ld_mask : nullptr, i0, end, ired);
+      for (int c = lane; c < p.n_chunks; c += G)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += p.scores[((int64_t)q * p.n_chunks + c) * 4 + e];
+      group_sum<G, 4>(v, red);
+    } else if constexpr (G > 64) {
+      long_pair_terms<T, G>(p, q, i0, end, range, v, reinterpret_cast<double(*)[2]>(red), ired);
+    } else {
+      pair_terms<T, G>(p, q, i0, end, v);
+      group_sum<G, 4>(v, red);
+    }
     const double nw = p.mean ? fmax(v[1], 1.0) : 1.0, nl = p.mean ? fmax(v[3], 1.0) : 1.0;
     const double m = p.beta * (v[0] / nw - v[2] / nl) - p.margin;
     double loss, dm;
     pref_term(p, m, &loss, &dm);
     const double g = p.loss_scale * p.beta * dm;     // d loss / d s(win) = -d loss / d s(lose)
-    loss_sum += p.loss_scale * loss;
-    right += m > 0.0 ? 1.0 : 0.0;
-    m_sum += m;
-    bad = bad || !isfinite(g);
-    if (threadIdx.x == 0) {
+    const T g_side[2] = {(T)(g / nw), (T)(-g / nl)};
+    if (lane == 0 && i0 == 0) {
+      sums[0] += p.loss_scale * loss;
+      sums[1] += m > 0.0 ? 1.0 : 0.0;
+      sums[2] += m;
       if (p.margins) p.margins[q] = m;
       if (p.side[0].adv) {
         p.side[0].adv[q * p.adv_stride] = (float)-g;
         p.side[1].adv[q * p.adv_stride] = (float)g;
       }
+      bad = bad || !isfinite((float)g) || !isfinite(g_side[0]) || !isfinite(g_side[1]);
     }
-    if (p.side[0].grad) {
+    if (!p.side[0].grad) continue;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const PrefSide& s = p.side[k];
-        const T o = (T)(k ? -g / nl : g / nw);
-        for (int i = threadIdx.x; i < p.L; i += kThreads)
-          static_cast<T*>(s.grad)[q * s.ld_grad + i] = !s.mask || s.mask[q * s.ld_mask + i] ? o : (T)0;
+    for (int c = 0; c < 2; ++c) {
+      const PrefSide& s = p.side[c];
+      if constexpr (G > 64) {
+        range_gradient<T, G>(p, s, q, i0, end, range[c], g_side[c]);
+      } else {
+        const uint8_t* mask = s.mask ? s.mask + q * s.ld_mask : nullptr;
+        T* grad = static_cast<T*>(s.grad) + q * s.ld_grad;
+        for (int j = i0; j < end; j += G * 4) {
+          Positions<G, 4> pos;
+          pos.load(mask, j + lane, end);
+          T o[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) o[u] = pos.live[u] ? g_side[c] : (T)0;
+          pos.store(grad, j + lane, end, o);
+        }
       }
     }
   }
-  if (bad && p.flags && threadIdx.x == 0) atomicOr(p.flags, kFlagNonfinite);
-  if (threadIdx.x == 0) {
-    p.part[blockIdx.x] = make_double2(loss_sum, right);
-    p.msum[blockIdx.x] = m_sum;
-  }
+}
+
+__device__ void write_pref_stats(const PrefArgs& p, const double (&s)[kPrefSums]) {
+#pragma unroll
+  for (int i = 0; i < kPrefSums; ++i) p.stats[i] = s[i];
+  if (!isfinite(s[0]) && p.flags) atomicOr(p.flags, kFlagNonfinite);
+}
+
+template <typename T, int G>
+__global__ __launch_bounds__(kThreads) void k_preference_scores(PrefArgs p) {
+  constexpr int kWg = kThreads, kGroups = kWg / G;
+  __shared__ double red[kWg / 64][2];
+  __shared__ int ired[kWg / 64][3];
+  scores_pass<T, G>(p, blockIdx.x * kGroups + group_index<G, kWg>(), gridDim.x * kGroups, red, ired);
+}
+
+template <typename T, int G>
+__global__ __launch_bounds__(kThreads) void k_preference(PrefArgs p) {
+  constexpr int kWg = kThreads, kGroups = kWg / G;
+  __shared__ double red[kWg / 64][4];
+  double sums[kPrefSums] = {0.0, 0.0, 0.0};
+  bool bad = false;
+  __shared__ int ired[kWg / 64][3];
+  pairs_pass<T, G>(p, blockIdx.x * kGroups + group_index<G, kWg>(), gridDim.x * kGroups, sums, bad, red, ired);
+  if (bad && p.flags) atomicOr(p.flags, kFlagNonfinite);
+  group_sum<kWg, kPrefSums>(sums, reinterpret_cast<double(*)[kPrefSums]>(red));
+  if (threadIdx.x == 0)
+#pragma unroll
+    for (int i = 0; i < kPrefSums; ++i) p.part[blockIdx.x * kPrefSums + i] = sums[i];
 }
 
 __global__ __launch_bounds__(kThreads) void k_preference_stats(PrefArgs p, int wgs) {
-  __shared__ double red[kThreads / 64][3];
-  double s[3] = {0.0, 0.0, 0.0};
-  for (int i = threadIdx.x; i < wgs; i += kThreads) {
-    s[0] += p.part[i].x;
-    s[1] += p.part[i].y;
-    s[2] += p.msum[i];
+  __shared__ double red[kThreads / 64][kPrefSums];
+  double s[kPrefSums] = {0.0, 0.0, 0.0};
+#pragma unroll 4
+  for (int i = threadIdx.x; i < wgs; i += kThreads)
+#pragma unroll
+    for (int c = 0; c < kPrefSums; ++c) s[c] += p.part[i * kPrefSums + c];
+  group_sum<kThreads, kPrefSums>(s, red);
+  if (threadIdx.x == 0) write_pref_stats(p, s);
+}
+
+// A small batch of pairs in one launch of one workgroup.
+template <typename T, int G>
+__global__ __launch_bounds__(kSmallThreads) void k_preference_small(PrefArgs p) {
+  constexpr int kGroups = kSmallThreads / G;
+  __shared__ double red[kSmallThreads / 64][kPrefSums];
+  if (p.scores) {
+    scores_pass<T, G>(p, group_index<G, kSmallThreads>(), kGroups, nullptr, nullptr);
+    __syncthreads();
   }
-  wg_sum<3>(s, red);
-  if (threadIdx.x < 3) p.stats[threadIdx.x] = s[threadIdx.x];
-  if (threadIdx.x == 0 && !isfinite(s[0]) && p.flags) atomicOr(p.flags, kFlagNonfinite);
+  double sums[kPrefSums] = {0.0, 0.0, 0.0};
+  bool bad = false;
+  pairs_pass<T, G>(p, group_index<G, kSmallThreads>(), kGroups, sums, bad, nullptr, nullptr);
+  if (bad && p.flags) atomicOr(p.flags, kFlagNonfinite);
+  group_sum<kSmallThreads, kPrefSums>(sums, red);
+  if (threadIdx.x == 0) write_pref_stats(p, sums);
 }
 
 static int check_preference(const bgpo_preference* p) {
@@ -339,19 +1150,48 @@ static int check_preference(const bgpo_preference* p) {
       !isfinite(p->loss_scale) || !(p->label_smoothing >= 0.0 && p->label_smoothing < 1.0) ||
       (p->label_smoothing != 0.0 && p->kind != BGPO_PREF_SIGMOID))
     return BGPO_ERR_INVALID_ARG;
-  if ((int64_t)p->P * p->L > int64_t(1) << 39) return BGPO_ERR_UNSUPPORTED;
+  if (p->L > 1 << 30 || (int64_t)p->P * p->L > int64_t(1) << 39) return BGPO_ERR_UNSUPPORTED;
   return BGPO_OK;
 }
 
-static size_t preference_bytes() { return kMaxWgs * 3 * sizeof(double); }
+static PolicyPlan plan_preference(const bgpo_preference* p) {
+  PolicyPlan q;
+  cut_rows(p->P, p->L, &q);
+  q.rows_pass = q.n_chunks > 1;
+  return q;
+}
 
-template <typename T>
-static int run_preference(const PrefArgs& p, hipStream_t s) {
-  const unsigned wgs = (unsigned)std::min<int64_t>(p.P, kMaxWgs);
-  k_preference<T><<<wgs, kThreads, 0, s>>>(p);
+static size_t preference_bytes(const PolicyPlan& q) {
+  return (q.n_chunks > 1 ? (size_t)q.pieces * 4 * sizeof(double) : 0) +
+         (q.small ? 0 : kMaxWgs * kPrefSums * sizeof(double)) + 256;
+}
+
+template <typename T, int G>
+static int launch_preference(const PrefArgs& p, const PolicyPlan& q, hipStream_t s) {
+  constexpr int kWg = kThreads, kGroups = kWg / G;
+  const unsigned wgs = (unsigned)std::min<int64_t>((q.pieces + kGroups - 1) / kGroups, kMaxWgs);
+  if (p.scores) {
+    k_preference_scores<T, G><<<wgs, kWg, 0, s>>>(p);
+    if (hipGetLastError() != hipSuccess) return BGPO_ERR_HIP;
+  }
+  k_preference<T, G><<<wgs, kWg, 0, s>>>(p);
   if (hipGetLastError() != hipSuccess) return BGPO_ERR_HIP;
   k_preference_stats<<<1, kThreads, 0, s>>>(p, (int)wgs);
   return hipGetLastError() == hipSuccess ? BGPO_OK : BGPO_ERR_HIP;
+}
+
+template <typename T>
+static int run_preference(const PrefArgs& p, const PolicyPlan& q, hipStream_t s) {
+  if (q.small) {
+    if (q.lanes == 16) k_preference_small<T, 16><<<1, kSmallThreads, 0, s>>>(p);
+    else k_preference_small<T, 64><<<1, kSmallThreads, 0, s>>>(p);
+    return hipGetLastError() == hipSuccess ? BGPO_OK : BGPO_ERR_HIP;
+  }
+  switch (q.lanes) {
+    case 16: return launch_preference<T, 16>(p, q, s);
+    case 64: return launch_preference<T, 64>(p, q, s);
+    default: return launch_preference<T, kThreads>(p, q, s);
+  }
 }
 
 }  // namespace bgpo
@@ -364,7 +1204,7 @@ int bgpo_policy_workspace_size(const bgpo_policy* prob, size_t* bytes) {
   const int st = check_policy(prob);
   if (st != BGPO_OK) return st;
   if (!bytes) return BGPO_ERR_INVALID_ARG;
-  *bytes = policy_bytes(prob);
+  *bytes = policy_bytes(plan_policy(prob));
   return BGPO_OK;
 }
 
@@ -389,24 +1229,29 @@ int bgpo_policy_loss(const bgpo_policy* prob, const void* logp, const void* logp
                       prob->ld_adv ? Array{adv, B, prob->ld_adv, L, 4} : vec(adv, B, 4)};
   const Array out[] = {{dlogp, B, prob->ld_dlogp, L, e}, vec(stats, BGPO_POLICY_STATS, 8), vec(status_flags, 1, 4)};
   if (any_overlap(out, in)) return BGPO_ERR_INVALID_ARG;
-  if (!workspace || ws_bytes < policy_bytes(prob) || misaligned(workspace, 256)) return BGPO_ERR_WORKSPACE;
+  const PolicyPlan q = plan_policy(prob);
+  if (!workspace || ws_bytes < policy_bytes(q) || misaligned(workspace, 256)) return BGPO_ERR_WORKSPACE;
   PolicyArgs p{logp, logp_old, logp_ref, adv, resp_mask, dlogp, stats, status_flags,
                prob->ld_logp, prob->ld_old, prob->ld_ref, prob->ld_mask, prob->ld_dlogp, prob->ld_adv,
                prob->B, prob->L, prob->ratio, prob->reduce, prob->kl,
                1.0 - prob->clip_low, 1.0 + prob->clip_high, prob->clip_dual, prob->kl_coef, prob->loss_scale};
-  p.rows = static_cast<double2*>(workspace);
-  p.counts = reinterpret_cast<double*>(p.rows + B);
+  p.chunk = q.chunk;
+  p.n_chunks = q.n_chunks;
+  p.rows = q.rows_pass ? static_cast<double2*>(workspace) : nullptr;
+  p.counts = static_cast<double*>(workspace) + (q.rows_pass ? 2 * q.pieces : 0);
   p.part = p.counts + kMaxWgs;
   p.count_wgs = 0;
   hipStream_t s = (hipStream_t)stream;
-  return e == 8 ? run_policy<double>(p, s) : run_policy<float>(p, s);
+  const bool token = prob->ratio == BGPO_RATIO_TOKEN;
+  return e == 8 ? (token ? run_policy<double, true>(p, q, s) : run_policy<double, false>(p, q, s))
+                : (token ? run_policy<float, true>(p, q, s) : run_policy<float, false>(p, q, s));
 }
 
 int bgpo_preference_workspace_size(const bgpo_preference* prob, size_t* bytes) {
   const int st = check_preference(prob);
   if (st != BGPO_OK) return st;
   if (!bytes) return BGPO_ERR_INVALID_ARG;
-  *bytes = preference_bytes();
+  *bytes = preference_bytes(plan_preference(prob));
   return BGPO_OK;
 }
 
@@ -438,16 +1283,19 @@ int bgpo_preference_loss(const bgpo_preference* prob, const void* win, const voi
                        {adv_lose, P, as, 1, 4}, vec(margins, P, 8), vec(stats, BGPO_PREF_STATS, 8),
                        vec(status_flags, 1, 4)};
   if (any_overlap(out, in)) return BGPO_ERR_INVALID_ARG;
-  if (!workspace || ws_bytes < preference_bytes() || misaligned(workspace, 256)) return BGPO_ERR_WORKSPACE;
+  const PolicyPlan q = plan_preference(prob);
+  if (!workspace || ws_bytes < preference_bytes(q) || misaligned(workspace, 256)) return BGPO_ERR_WORKSPACE;
   PrefArgs p{{{win, win_ref, win_mask, dwin, adv_win, prob->ld_win, prob->ld_win_ref, prob->ld_win_mask, prob->ld_dwin},
               {lose, lose_ref, lose_mask, dlose, adv_lose, prob->ld_lose, prob->ld_lose_ref, prob->ld_lose_mask,
                prob->ld_dlose}},
              margins, stats, status_flags, as, prob->P, prob->L, prob->kind, prob->mean,
              prob->beta, prob->margin, prob->label_smoothing, prob->loss_scale};
-  p.part = static_cast<double2*>(workspace);
-  p.msum = reinterpret_cast<double*>(p.part + kMaxWgs);
+  p.chunk = q.chunk;
+  p.n_chunks = q.n_chunks;
+  p.scores = q.n_chunks > 1 ? static_cast<double*>(workspace) : nullptr;
+  p.part = static_cast<double*>(workspace) + (q.n_chunks > 1 ? 4 * q.pieces : 0);
   hipStream_t s = (hipStream_t)stream;
-  return e == 8 ? run_preference<double>(p, s) : run_preference<float>(p, s);
+  return e == 8 ? run_preference<double>(p, q, s) : run_preference<float>(p, q, s);
 }
 
 }  // extern "C"

@@ -131,7 +131,7 @@ def _policy_loss(b, prob, over=()):
     (dict(clip_low=math.nan), INVALID), (dict(clip_high=-0.1), INVALID), (dict(clip_high=math.nan), INVALID),
     (dict(clip_dual=1.0), INVALID), (dict(clip_dual=-2.0), INVALID), (dict(clip_dual=math.inf), INVALID),
     (dict(kl_coef=math.nan), INVALID), (dict(loss_scale=math.inf), INVALID), (dict(ld_adv=-1), INVALID),
-    (dict(ratio=1, ld_adv=128), INVALID), (dict(B=1 << 21, L=1 << 20), UNSUPPORTED)])
+    (dict(ratio=1, ld_adv=128), INVALID), (dict(B=1 << 21, L=1 << 20), UNSUPPORTED), (dict(B=1, L=(1 << 30) + 1), UNSUPPORTED)])
 def test_policy_problems(b, kw, status):
     n = ctypes.c_size_t(0)
     p = _policy(b, **kw)
@@ -190,7 +190,7 @@ def _pref_loss(b, prob, over=()):
     (dict(beta=0.0), INVALID), (dict(beta=-1.0), INVALID), (dict(beta=math.inf), INVALID), (dict(beta=math.nan), INVALID),
     (dict(margin=math.nan), INVALID), (dict(loss_scale=math.inf), INVALID), (dict(label_smoothing=-0.1), INVALID),
     (dict(label_smoothing=1.0), INVALID), (dict(label_smoothing=0.1, kind=1), INVALID),
-    (dict(P=1 << 20, L=1 << 20), UNSUPPORTED)])
+    (dict(P=1 << 20, L=1 << 20), UNSUPPORTED), (dict(P=1, L=(1 << 30) + 1), UNSUPPORTED)])
 def test_preference_problems(b, kw, status):
     n = ctypes.c_size_t(0)
     p = _pref(b, **kw)
