@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -81,6 +82,13 @@ class _Preference(ctypes.Structure):
                 [(k, ctypes.c_int32) for k in ("P", "L", "dtype", "kind", "mean", "reserved")])
 
 
+# the same structures as bytes (passed as they are: a third of the time that a
+# ctypes structure takes to build)
+_POLICY = struct.Struct("6q5d6i")
+_PREFERENCE = struct.Struct("9q4d6i")
+assert _POLICY.size == ctypes.sizeof(_Policy) and _PREFERENCE.size == ctypes.sizeof(_Preference)
+
+
 class Timing(ctypes.Structure):
     """Per-kernel-class elapsed milliseconds and launch counts (bgpo_timing)."""
     _fields_ = [("ms", ctypes.c_double * len(KERNEL_CLASSES)),
@@ -123,9 +131,9 @@ def _load():
     lib.bgpo_logits_logp.argtypes = [P(_Logits), vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.bgpo_logits_logp_bwd.argtypes = [P(_Logits), vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_int64, vp]
     lib.bgpo_policy_workspace_size.argtypes = [P(_Policy), P(sz)]
-    lib.bgpo_policy_loss.argtypes = [P(_Policy)] + [vp] * 9 + [sz, vp]
+    lib.bgpo_policy_loss.argtypes = [vp] * 10 + [sz, vp]
     lib.bgpo_preference_workspace_size.argtypes = [P(_Preference), P(sz)]
-    lib.bgpo_preference_loss.argtypes = [P(_Preference)] + [vp] * 14 + [sz, vp]
+    lib.bgpo_preference_loss.argtypes = [vp] * 15 + [sz, vp]
     lib.bgpo_grad_workspace_size.restype = sz
     lib.bgpo_grad_workspace_size.argtypes = []
     lib.bgpo_grad_norm.argtypes = [P(_Tensor), i32, i32, vp, vp, vp, sz, vp]
@@ -432,41 +440,43 @@ _F32 = (torch.float32,)
 _U8 = (torch.uint8, torch.bool)
 
 
-def _on_current_device(t, name: str):
+def _device(t) -> int:
+    """The current device (of a CPU tensor's call, which is refused: none)."""
+    return torch.cuda.current_device() if t is not None and t.is_cuda else -2
+
+
+def _refuse(t, name: str, dtypes, shape, device: int):
+    """Raises for the first thing that is wrong with a tensor."""
+    if t is None:
+        raise ValueError(f"{name} is required")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
-    if t.get_device() != torch.cuda.current_device():
+    if t.get_device() != device:
         raise ValueError(f"{name} is on another device than the current one")
-
-
-def _vec(t: Optional[torch.Tensor], name: str, dtypes, n, allow_none=False):
-    """The address of a contiguous tensor of n elements on the current device."""
-    if t is None:
-        if allow_none:
-            return None
-        raise ValueError(f"{name} is required")
-    _on_current_device(t, name)
     if t.dtype not in dtypes:
         raise ValueError(f"{name} has dtype {t.dtype}, expected one of {dtypes}")
-    if t.dim() != 1 or t.shape[0] != n:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(n,)}")
-    if not t.is_contiguous():
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    if len(shape) == 1:
         raise ValueError(f"{name} must be contiguous")
+
+
+def _vec(t: Optional[torch.Tensor], name: str, dtypes, n, device: int, allow_none=False):
+    """The address of a contiguous tensor of n elements on the current device."""
+    if t is None and allow_none:
+        return None
+    if t is None or t.get_device() != device or t.dtype not in dtypes or t.shape != (n,) or not t.is_contiguous():
+        _refuse(t, name, dtypes, (n,), device)
     return t.data_ptr()
 
 
-def _mat(t: Optional[torch.Tensor], name: str, dtypes, rows: int, cols: int, allow_none=False):
+def _mat(t: Optional[torch.Tensor], name: str, dtypes, rows: int, cols: int, device: int, allow_none=False):
     """(address, elements between rows) of a matrix with contiguous rows on the
     current device."""
-    if t is None:
-        if allow_none:
-            return None, 0
-        raise ValueError(f"{name} is required")
-    _on_current_device(t, name)
-    if t.dtype not in dtypes:
-        raise ValueError(f"{name} has dtype {t.dtype}, expected one of {dtypes}")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(rows, cols)}")
+    if t is None and allow_none:
+        return None, 0
+    if t is None or t.get_device() != device or t.dtype not in dtypes or t.shape != (rows, cols):
+        _refuse(t, name, dtypes, (rows, cols), device)
     ld, inner = t.stride()
     if inner != 1 and cols > 1:
         raise ValueError(f"{name} must have contiguous rows")
@@ -477,21 +487,22 @@ def _mat(t: Optional[torch.Tensor], name: str, dtypes, rows: int, cols: int, all
     return t.data_ptr(), ld
 
 
-def _workspace_args(ws: Optional[torch.Tensor]):
+def _workspace_args(ws: Optional[torch.Tensor], device: int):
     """(address, bytes) of a workspace; None is one of no bytes."""
     if ws is None:
         return None, 0
-    return _vec(ws, "workspace", (torch.uint8,), ws.numel()), ws.numel()
+    n = ws.numel()
+    return _vec(ws, "workspace", (torch.uint8,), n, device), n
 
 
-def _logits_problem(logits, scale: float, name="logits"):
+def _logits_problem(logits, scale: float, device: int):
     if logits.dim() != 2:
-        raise ValueError(f"{name} must be a matrix [rows, V]")
+        raise ValueError("logits must be a matrix [rows, V]")
     rows, V = logits.shape
     if rows == 0 or V == 0:
         ld = V
     else:
-        _, ld = _mat(logits, name, (torch.bfloat16, torch.float32), rows, V)
+        _, ld = _mat(logits, "logits", (torch.bfloat16, torch.float32), rows, V, device)
     return _Logits(rows, ld, V, BGPO_F32 if logits.dtype == torch.float32 else BGPO_BF16, scale, 0)
 
 
@@ -510,13 +521,14 @@ def logits_workspace(rows: int, V: int, device="cuda") -> torch.Tensor:
 def bgpo_logits_logp(logits, targets, logp, entropy=None, lse=None, workspace=None, row_mask=None, scale: float = 1.0,
                      stream=None):
     """Log-probability of each row's target (and the entropy and log-sum-exp)."""
-    prob = _logits_problem(logits, scale)
+    dev = _device(logits)
+    prob = _logits_problem(logits, scale, dev)
     n = prob.rows
-    ws, ws_bytes = _workspace_args(workspace)
+    ws, ws_bytes = _workspace_args(workspace, dev)
     _check(_lib.bgpo_logits_logp(
-        ctypes.byref(prob), logits.data_ptr(), _vec(targets, "targets", (torch.int32,), n),
-        _vec(row_mask, "row_mask", _U8, n, allow_none=True), _vec(logp, "logp", _F32, n),
-        _vec(entropy, "entropy", _F32, n, allow_none=True), _vec(lse, "lse", _F32, n, allow_none=True),
+        ctypes.byref(prob), logits.data_ptr(), _vec(targets, "targets", (torch.int32,), n, dev),
+        _vec(row_mask, "row_mask", _U8, n, dev, allow_none=True), _vec(logp, "logp", _F32, n, dev),
+        _vec(entropy, "entropy", _F32, n, dev, allow_none=True), _vec(lse, "lse", _F32, n, dev, allow_none=True),
         ws, ws_bytes, _stream(stream)), "bgpo_logits_logp")
 
 
@@ -524,14 +536,15 @@ def bgpo_logits_logp_bwd(logits, targets, lse, entropy, dlogp, dentropy, dlogits
                          stream=None):
     """Gradient of the logits from those of logp and the entropy; dlogits may be
     logits itself."""
-    prob = _logits_problem(logits, scale)
+    dev = _device(logits)
+    prob = _logits_problem(logits, scale, dev)
     n = prob.rows
-    out, ld_out = _mat(dlogits, "dlogits", (logits.dtype,), n, prob.V)
+    out, ld_out = _mat(dlogits, "dlogits", (logits.dtype,), n, prob.V, dev)
     _check(_lib.bgpo_logits_logp_bwd(
-        ctypes.byref(prob), logits.data_ptr(), _vec(targets, "targets", (torch.int32,), n),
-        _vec(row_mask, "row_mask", _U8, n, allow_none=True), _vec(lse, "lse", _F32, n),
-        _vec(entropy, "entropy", _F32, n, allow_none=True), _vec(dlogp, "dlogp", _F32, n),
-        _vec(dentropy, "dentropy", _F32, n, allow_none=True), out, ld_out, _stream(stream)),
+        ctypes.byref(prob), logits.data_ptr(), _vec(targets, "targets", (torch.int32,), n, dev),
+        _vec(row_mask, "row_mask", _U8, n, dev, allow_none=True), _vec(lse, "lse", _F32, n, dev),
+        _vec(entropy, "entropy", _F32, n, dev, allow_none=True), _vec(dlogp, "dlogp", _F32, n, dev),
+        _vec(dentropy, "dentropy", _F32, n, dev, allow_none=True), out, ld_out, _stream(stream)),
         "bgpo_logits_logp_bwd")
 
 
@@ -573,23 +586,24 @@ def bgpo_policy_loss(prob: PolicyLoss, logp, logp_old, logp_ref, adv, resp_mask,
                      status_flags=None, stream=None):
     """Clipped policy loss with a KL term, and its gradient dlogp (None: the loss
     alone); logp_old None: on-policy, logp_ref None: no KL term."""
-    B, L = prob.B, prob.L
-    lp, ld_logp = _mat(logp, "logp", _FLOATS, B, L)
+    B, L, dev = prob.B, prob.L, _device(logp)
+    lp, ld_logp = _mat(logp, "logp", _FLOATS, B, L, dev)
     t = (logp.dtype,)
-    old, ld_old = _mat(logp_old, "logp_old", t, B, L, allow_none=True)
-    ref, ld_ref = _mat(logp_ref, "logp_ref", t, B, L, allow_none=True)
-    mask, ld_mask = _mat(resp_mask, "resp_mask", _U8, B, L)
-    dl, ld_dlogp = _mat(dlogp, "dlogp", t, B, L, allow_none=True)
+    old, ld_old = _mat(logp_old, "logp_old", t, B, L, dev, allow_none=True)
+    ref, ld_ref = _mat(logp_ref, "logp_ref", t, B, L, dev, allow_none=True)
+    mask, ld_mask = _mat(resp_mask, "resp_mask", _U8, B, L, dev)
+    dl, ld_dlogp = _mat(dlogp, "dlogp", t, B, L, dev, allow_none=True)
     if adv is not None and adv.dim() == 2:
-        a, ld_adv = _mat(adv, "adv", _F32, B, L)
+        a, ld_adv = _mat(adv, "adv", _F32, B, L, dev)
     else:
-        a, ld_adv = _vec(adv, "adv", _F32, B), 0
-    ws, ws_bytes = _workspace_args(workspace)
+        a, ld_adv = _vec(adv, "adv", _F32, B, dev), 0
+    ws, ws_bytes = _workspace_args(workspace, dev)
     _check(_lib.bgpo_policy_loss(
-        ctypes.byref(prob.c((ld_logp, ld_old, ld_ref, ld_mask, ld_dlogp, ld_adv),
-                            BGPO_F64 if logp.dtype == torch.float64 else BGPO_F32)),
-        lp, old, ref, a, mask, dl, _vec(stats, "stats", (torch.float64,), BGPO_POLICY_STATS),
-        _vec(status_flags, "status_flags", (torch.int32,), 1, allow_none=True), ws, ws_bytes, _stream(stream)),
+        _POLICY.pack(ld_logp, ld_old, ld_ref, ld_mask, ld_dlogp, ld_adv, prob.clip_low, prob.clip_high, prob.clip_dual,
+                     prob.kl_coef, prob.loss_scale, B, L, BGPO_F64 if logp.dtype == torch.float64 else BGPO_F32,
+                     prob.ratio, prob.reduce, prob.kl),
+        lp, old, ref, a, mask, dl, _vec(stats, "stats", (torch.float64,), BGPO_POLICY_STATS, dev),
+        _vec(status_flags, "status_flags", (torch.int32,), 1, dev, allow_none=True), ws, ws_bytes, _stream(stream)),
         "bgpo_policy_loss")
 
 
@@ -628,48 +642,52 @@ def bgpo_preference_loss(prob: PreferenceLoss, win, lose, win_ref, lose_ref, win
     """Preference loss on paired log ratios and its gradient.  adv_win and
     adv_lose (vectors of one stride) are the advantages that send it through
     bgpo_elbo_bwd_accumulate with bound BGPO_BOUND_TAYLOR and loss scale 1."""
-    P, L = prob.P, prob.L
-    w, ld_w = _mat(win, "win", _FLOATS, P, L)
+    P, L, dev = prob.P, prob.L, _device(win)
+    w, ld_w = _mat(win, "win", _FLOATS, P, L, dev)
     t = (win.dtype,)
-    lo, ld_lo = _mat(lose, "lose", t, P, L)
-    wr, ld_wr = _mat(win_ref, "win_ref", t, P, L, allow_none=True)
-    lr, ld_lr = _mat(lose_ref, "lose_ref", t, P, L, allow_none=True)
-    wm, ld_wm = _mat(win_mask, "win_mask", _U8, P, L, allow_none=True)
-    lm, ld_lm = _mat(lose_mask, "lose_mask", _U8, P, L, allow_none=True)
-    dw, ld_dw = _mat(dwin, "dwin", t, P, L, allow_none=True)
-    dl, ld_dl = _mat(dlose, "dlose", t, P, L, allow_none=True)
+    lo, ld_lo = _mat(lose, "lose", t, P, L, dev)
+    wr, ld_wr = _mat(win_ref, "win_ref", t, P, L, dev, allow_none=True)
+    lr, ld_lr = _mat(lose_ref, "lose_ref", t, P, L, dev, allow_none=True)
+    wm, ld_wm = _mat(win_mask, "win_mask", _U8, P, L, dev, allow_none=True)
+    lm, ld_lm = _mat(lose_mask, "lose_mask", _U8, P, L, dev, allow_none=True)
+    dw, ld_dw = _mat(dwin, "dwin", t, P, L, dev, allow_none=True)
+    dl, ld_dl = _mat(dlose, "dlose", t, P, L, dev, allow_none=True)
     aw = al = None
     stride = 1
     if adv_win is not None or adv_lose is not None:
-        aw, al = (_mat(None if a is None else a[:, None] if a.dim() == 1 else a, name, _F32, P, 1, allow_none=True)
-                  for a, name in ((adv_win, "adv_win"), (adv_lose, "adv_lose")))
-        if P > 1 and None not in (aw[0], al[0]) and aw[1] != al[1]:
+        for a, name in ((adv_win, "adv_win"), (adv_lose, "adv_lose")):
+            if a is None or a.get_device() != dev or a.dtype not in _F32 or a.shape != (P,):
+                _refuse(a, name, _F32, (P,), dev)
+        stride = adv_win.stride(0)
+        if P > 1 and adv_lose.stride(0) != stride:
             raise ValueError("adv_win and adv_lose have different strides")
-        stride, aw, al = aw[1], aw[0], al[0]
-    ws, ws_bytes = _workspace_args(workspace)
+        aw, al = adv_win.data_ptr(), adv_lose.data_ptr()
+    ws, ws_bytes = _workspace_args(workspace, dev)
     _check(_lib.bgpo_preference_loss(
-        ctypes.byref(prob.c((ld_w, ld_lo, ld_wr, ld_lr, ld_wm, ld_lm, ld_dw, ld_dl, stride),
-                            BGPO_F64 if win.dtype == torch.float64 else BGPO_F32)),
-        w, lo, wr, lr, wm, lm, dw, dl, _vec(margins, "margins", (torch.float64,), P, allow_none=True), aw, al,
-        _vec(stats, "stats", (torch.float64,), BGPO_PREF_STATS),
-        _vec(status_flags, "status_flags", (torch.int32,), 1, allow_none=True), ws, ws_bytes, _stream(stream)),
+        _PREFERENCE.pack(ld_w, ld_lo, ld_wr, ld_lr, ld_wm, ld_lm, ld_dw, ld_dl, stride, prob.beta, prob.margin,
+                         prob.label_smoothing, prob.loss_scale, P, L,
+                         BGPO_F64 if win.dtype == torch.float64 else BGPO_F32, prob.kind, int(prob.mean), 0),
+        w, lo, wr, lr, wm, lm, dw, dl, _vec(margins, "margins", (torch.float64,), P, dev, allow_none=True), aw, al,
+        _vec(stats, "stats", (torch.float64,), BGPO_PREF_STATS, dev),
+        _vec(status_flags, "status_flags", (torch.int32,), 1, dev, allow_none=True), ws, ws_bytes, _stream(stream)),
         "bgpo_preference_loss")
 
 
 class GradList:
     """A list of gradients in the form that bgpo_grad_norm and bgpo_grad_clip
     take; keeps the tensors.  Built once and used again: every call looks up
-    where the tensors are and how large."""
+    where the tensors are, and takes in anew what has moved."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
         for i, t in enumerate(self.tensors):
-            _on_current_device(t, f"gradient {i}")
-            if t.dtype not in (torch.bfloat16, torch.float32):
-                raise ValueError(f"gradient {i} has dtype {t.dtype}, expected bfloat16 or float32")
+            if t.get_device() != _device(t) or t.dtype not in (torch.bfloat16, torch.float32):
+                _refuse(t, f"gradient {i}", (torch.bfloat16, torch.float32), tuple(t.shape), _device(t))
             if not t.is_contiguous():
                 raise ValueError(f"gradient {i} must be contiguous")
         self._at = self._where()
+        # (kept, so that an address seen again is the same memory)
+        self._storage = [t.untyped_storage() for t in self.tensors]
         self._c = (_Tensor * max(1, len(self.tensors)))(
             *[_Tensor(t.data_ptr(), t.numel(), BGPO_F32 if t.dtype == torch.float32 else BGPO_BF16, 0)
               for t in self.tensors])
@@ -678,7 +696,7 @@ class GradList:
         return len(self.tensors)
 
     def _where(self):
-        return [(t.data_ptr(), t.numel()) for t in self.tensors]
+        return list(map(torch.Tensor.data_ptr, self.tensors))
 
     def c(self):
         if self._at != self._where():
@@ -693,9 +711,10 @@ def grad_workspace(device="cuda") -> torch.Tensor:
 
 def bgpo_grad_norm(grads: GradList, norm, workspace, norm_type: int = BGPO_NORM_L2, status_flags=None, stream=None):
     """norm[0] = the norm of all gradients of the list as one vector."""
-    ws, ws_bytes = _workspace_args(workspace)
-    _check(_lib.bgpo_grad_norm(grads.c(), len(grads), norm_type, _vec(norm, "norm", (torch.float64,), 1),
-                               _vec(status_flags, "status_flags", (torch.int32,), 1, allow_none=True), ws, ws_bytes,
+    dev = _device(norm)
+    ws, ws_bytes = _workspace_args(workspace, dev)
+    _check(_lib.bgpo_grad_norm(grads.c(), len(grads), norm_type, _vec(norm, "norm", (torch.float64,), 1, dev),
+                               _vec(status_flags, "status_flags", (torch.int32,), 1, dev, allow_none=True), ws, ws_bytes,
                                _stream(stream)), "bgpo_grad_norm")
 
 
@@ -704,8 +723,9 @@ def bgpo_grad_clip(grads: GradList, max_norm: float, norm, out: Optional[GradLis
     place, or into the tensors of `out`."""
     if out is not None and len(out) != len(grads):
         raise ValueError(f"out has {len(out)} tensors, expected {len(grads)}")
+    dev = _device(norm)
     _check(_lib.bgpo_grad_clip(grads.c(), None if out is None else out.c(), len(grads), float(max_norm),
-                               _vec(norm, "norm", (torch.float64,), 1), _stream(stream)), "bgpo_grad_clip")
+                               _vec(norm, "norm", (torch.float64,), 1, dev), _stream(stream)), "bgpo_grad_clip")
 
 
 def bgpo_test_gemm_nt(A, B, C, stream=None):

@@ -1,13 +1,16 @@
 // Norm of a list of gradients, and their scaling to a largest norm.
 //
-// The list travels in the kernels' arguments, kTable entries to a launch.  Its
-// tensors are cut into chunks of kChunk elements, numbered through the launch;
-// a workgroup finds its chunk's tensor by bisection.
+// The list travels in the kernels' arguments, up to kEntries tensors to a launch
+// (12 bytes each: an address of 48 bits, the elements of the last chunk, the type,
+// and the number of the first chunk).  The tensors are cut into chunks of kChunk
+// elements, numbered through the launch; a workgroup finds its chunk's tensor by
+// bisection.
 #include <math.h>
 
 #include <algorithm>
 #include <memory>
 #include <new>
+#include <type_traits>
 
 #include "../../include/bgpo.h"
 #include "../../include/bgpo_grads.h"
@@ -17,34 +20,60 @@
 
 namespace bgpo {
 
-constexpr int kTable = 112;                // entries of a launch (3.7 KB of arguments)
 constexpr int64_t kChunk = 16384;
-constexpr int kNormWgs = 2048;             // workgroups of a norm pass, one partial each
+constexpr int kNormWgs = 1024;             // workgroups of a norm pass, one partial each
 constexpr int kMaxClipWgs = 1 << 22;
+constexpr int kEntries = 312, kPairs = 184;  // of a launch: gradients; gradients and outputs (4 KB of arguments)
 
 // 16 bytes at the alignment of the element type
 typedef uint32_t raw16 __attribute__((ext_vector_type(4), aligned(2), may_alias));
 typedef uint32_t raw8 __attribute__((ext_vector_type(2), aligned(2), may_alias));
 
+// A tensor: its address, elements of its last chunk less one, whether fp32.
+struct Packed {
+  uint64_t v;
+  __host__ __device__ const void* data() const { return reinterpret_cast<const void*>(v >> 16); }
+  __host__ __device__ bool f32() const { return v >> 15 & 1; }
+  __host__ __device__ int tail() const { return (int)(v & 0x3FFF) + 1; }
+  static Packed of(const bgpo_tensor& t) {
+    return Packed{(uint64_t)(uintptr_t)t.data << 16 | (uint64_t)(t.dtype == BGPO_F32) << 15 |
+                  (uint64_t)((t.n - 1) % kChunk)};
+  }
+};
+static_assert(kChunk <= 1 << 14, "a chunk's elements are held in 14 bits");
+
+template <int N, bool OUT>
 struct Table {
-  const void* src[kTable];
-  void* dst[kTable];
-  int64_t n[kTable];
-  uint32_t first[kTable];                  // number of its first chunk
-  uint8_t src_f32[kTable], dst_f32[kTable];
-  uint32_t chunks;
+  Packed src[N];
+  Packed dst[OUT ? N : 1];
+  uint32_t first[N + 1];                   // number of the first chunk of each, and of all
   int count;
+
+  __device__ uint32_t chunks() const { return first[count]; }
+  // the entry that holds chunk c
+  __device__ __forceinline__ int find(uint32_t c) const {
+    int lo = 0, hi = count - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (first[mid] <= c) lo = mid;
+      else hi = mid - 1;
+    }
+    return lo;
+  }
+  // where chunk c of entry e starts and how long it is
+  __device__ __forceinline__ int64_t start(int e, uint32_t c) const { return (int64_t)(c - first[e]) * kChunk; }
+  __device__ __forceinline__ int length(int e, uint32_t c) const { return c + 1 == first[e + 1] ? src[e].tail() : (int)kChunk; }
 };
 
-// the entry that holds chunk c
-__device__ __forceinline__ int find_entry(const Table& t, uint32_t c) {
-  int lo = 0, hi = t.count - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (t.first[mid] <= c) lo = mid;
-    else hi = mid - 1;
-  }
-  return lo;
+// Lists of this many bytes or more are past the 256 MB last-level cache: streamed
+// (non-temporal) accesses are faster there.  534M fp32 elements: the norm 354 us
+// without, 314 (6.8 TB/s) with; clipped into bf16, loads and stores, 586 and 545
+// (5.9 TB/s).  200 MB: no difference.
+constexpr int64_t kStreamBytes = int64_t(256) << 20;
+
+template <bool NT, typename V>
+__device__ __forceinline__ V load(const void* p) {
+  return NT ? __builtin_nontemporal_load(static_cast<const V*>(p)) : *static_cast<const V*>(p);
 }
 
 // Running norm of one thread: the sum of squares in float64, or the largest
@@ -77,27 +106,40 @@ struct Norm {
   }
 };
 
+// The loads of one chunk: U 16-byte groups of a lane at a time.
+template <bool MAX, bool F32, bool NT>
+__device__ __forceinline__ void add_chunk(Norm<MAX>& a, const void* p, int n) {
+  constexpr int N = F32 ? 4 : 8, U = 4;
+  typedef std::conditional_t<F32, float, bf16_t> T;
+  const T* x = static_cast<const T*>(p);
+  int i = (int)threadIdx.x * N;
+  for (; i + (U - 1) * 256 * N + N <= n; i += U * 256 * N) {
+    raw16 r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) r[u] = load<NT, raw16>(x + i + u * 256 * N);
+#pragma unroll
+    for (int u = 0; u < U; ++u) a.add16(r[u], F32);
+  }
+  for (; i + N <= n; i += 256 * N) a.add16(*reinterpret_cast<const raw16*>(x + i), F32);
+  i = n / N * N + (int)threadIdx.x;
+  if (i < n) {
+    if constexpr (F32) a.add(x[i]);
+    else a.add(bf16_to_f32(x[i]));
+  }
+}
+
 // Partial norms: workgroup k takes chunks k, k + grid, ..; the launches of a
 // longer list go on from the partials before.
-template <bool MAX>
-__global__ __launch_bounds__(256) void k_grad_norm(Table t, bool first, double* __restrict__ part) {
+template <bool MAX, bool NT>
+__global__ __launch_bounds__(256) void k_grad_norm(Table<kEntries, false> t, bool first, double* __restrict__ part) {
   __shared__ double red[4];
   Norm<MAX> a;
-  for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
-    const int e = find_entry(t, c);
-    const int64_t at = (int64_t)(c - t.first[e]) * kChunk;
-    const int n = (int)min(kChunk, t.n[e] - at);
-    if (t.src_f32[e]) {
-      const float* x = static_cast<const float*>(t.src[e]) + at;
-      for (int i = threadIdx.x * 4; i + 4 <= n; i += 1024) a.add16(*reinterpret_cast<const raw16*>(x + i), true);
-      const int i = (n & ~3) + threadIdx.x;
-      if (i < n) a.add(x[i]);
-    } else {
-      const bf16_t* x = static_cast<const bf16_t*>(t.src[e]) + at;
-      for (int i = threadIdx.x * 8; i + 8 <= n; i += 2048) a.add16(*reinterpret_cast<const raw16*>(x + i), false);
-      const int i = (n & ~7) + threadIdx.x;
-      if (i < n) a.add(bf16_to_f32(x[i]));
-    }
+  for (uint32_t c = blockIdx.x; c < t.chunks(); c += gridDim.x) {
+    const int e = t.find(c), n = t.length(e, c);
+    const int64_t at = t.start(e, c);
+    const char* p = static_cast<const char*>(t.src[e].data());
+    if (t.src[e].f32()) add_chunk<MAX, true, NT>(a, p + at * 4, n);
+    else add_chunk<MAX, false, NT>(a, p + at * 2, n);
   }
   double v = a.value();
 #pragma unroll
@@ -128,54 +170,93 @@ __global__ __launch_bounds__(256) void k_grad_norm_final(const double* __restric
   if (flags && !isfinite(v)) atomicOr(flags, kFlagNonfinite);
 }
 
-// One chunk after the other: dst = src * f, f = max_norm / norm where the norm
-// is larger (and finite), else 1.  An entry that is its own output is left
-// alone where f is 1.
-__global__ __launch_bounds__(256) void k_grad_clip(Table t, double max_norm, const double* __restrict__ norm) {
-  const double v = norm[0];
-  const float f = isfinite(v) && v > max_norm ? (float)(max_norm / v) : 1.f;
-  for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
-    const int e = find_entry(t, c);
-    if (f == 1.f && t.src[e] == t.dst[e]) continue;
-    const int64_t at = (int64_t)(c - t.first[e]) * kChunk;
-    const int n = (int)min(kChunk, t.n[e] - at);
-    const bool sf = t.src_f32[e], df = t.dst_f32[e];
-    const float* xf = static_cast<const float*>(t.src[e]) + at;
-    const bf16_t* xb = static_cast<const bf16_t*>(t.src[e]) + at;
-    float* of = static_cast<float*>(t.dst[e]) + at;
-    bf16_t* ob = static_cast<bf16_t*>(t.dst[e]) + at;
-    for (int i = threadIdx.x * 4; i + 4 <= n; i += 1024) {
-      float x[4];
-      if (sf) {
-        const raw16 r = *reinterpret_cast<const raw16*>(xf + i);
+// dst = src * f of one chunk, U groups of four elements of a lane at a time.
+template <bool SF, bool DF, bool NT>
+__device__ __forceinline__ void scale_chunk(const void* src, void* dst, int n, float f) {
+  constexpr int U = 8;
+  typedef std::conditional_t<SF, float, bf16_t> S;
+  typedef std::conditional_t<DF, float, bf16_t> D;
+  typedef std::conditional_t<SF, raw16, raw8> SV;
+  typedef std::conditional_t<DF, raw16, raw8> DV;
+  const S* x = static_cast<const S*>(src);
+  D* o = static_cast<D*>(dst);
+  auto scale = [&](const SV& r) {
+    float v[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = __uint_as_float(r[k]) * f;
-      } else {
-        const raw8 r = *reinterpret_cast<const raw8*>(xb + i);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          x[2 * k] = __uint_as_float(r[k] << 16) * f;
-          x[2 * k + 1] = __uint_as_float(r[k] & 0xFFFF0000u) * f;
-        }
-      }
-      if (df) {
-        raw16 r;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) r[k] = __float_as_uint(x[k]);
-        *reinterpret_cast<raw16*>(of + i) = r;
-      } else {
-        raw8 r;
-        r[0] = pack_bf16x2(x[0], x[1]);
-        r[1] = pack_bf16x2(x[2], x[3]);
-        *reinterpret_cast<raw8*>(ob + i) = r;
-      }
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (SF) v[k] = __uint_as_float(r[k]) * f;
+      else v[k] = __uint_as_float(k & 1 ? r[k / 2] & 0xFFFF0000u : r[k / 2] << 16) * f;
     }
-    const int i = (n & ~3) + threadIdx.x;
-    if (i < n) {
-      const float x = (sf ? xf[i] : bf16_to_f32(xb[i])) * f;
-      if (df) of[i] = x;
-      else ob[i] = f32_to_bf16(x);
+    DV w;
+    if constexpr (DF) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = __float_as_uint(v[k]);
+    } else {
+      w[0] = pack_bf16x2(v[0], v[1]);
+      w[1] = pack_bf16x2(v[2], v[3]);
     }
+    return w;
+  };
+  auto store = [&](int i, const DV& w) {
+    if (NT) __builtin_nontemporal_store(w, reinterpret_cast<DV*>(o + i));
+    else *reinterpret_cast<DV*>(o + i) = w;
+  };
+  int i = (int)threadIdx.x * 4;
+  for (; i + (U - 1) * 1024 + 4 <= n; i += U * 1024) {
+    SV r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) r[u] = load<NT, SV>(x + i + u * 1024);
+#pragma unroll
+    for (int u = 0; u < U; ++u) store(i + u * 1024, scale(r[u]));
+  }
+  for (; i + 4 <= n; i += 1024) store(i, scale(*reinterpret_cast<const SV*>(x + i)));
+  i = (n & ~3) + (int)threadIdx.x;
+  if (i < n) {
+    float v;
+    if constexpr (SF) v = x[i] * f;
+    else v = bf16_to_f32(x[i]) * f;
+    if constexpr (DF) o[i] = v;
+    else o[i] = f32_to_bf16(v);
+  }
+}
+
+// the factor: max_norm / norm where the norm is larger (and finite), else 1
+__device__ __forceinline__ float clip_factor(double max_norm, double v) {
+  return isfinite(v) && v > max_norm ? (float)(max_norm / v) : 1.f;
+}
+
+// In place.  Nothing is touched where the factor is 1.
+template <bool NT>
+__global__ __launch_bounds__(256) void k_grad_scale(Table<kEntries, false> t, double max_norm,
+                                                    const double* __restrict__ norm) {
+  const float f = clip_factor(max_norm, norm[0]);
+  if (f == 1.f) return;
+  const uint32_t n_chunks = t.chunks();
+  for (uint32_t c = blockIdx.x; c < n_chunks; c += gridDim.x) {
+    const int e = t.find(c), n = t.length(e, c);
+    const int64_t at = t.start(e, c);
+    char* p = static_cast<char*>(const_cast<void*>(t.src[e].data()));
+    if (t.src[e].f32()) scale_chunk<true, true, NT>(p + at * 4, p + at * 4, n, f);
+    else scale_chunk<false, false, NT>(p + at * 2, p + at * 2, n, f);
+  }
+}
+
+// Into the outputs.
+template <bool NT>
+__global__ __launch_bounds__(256) void k_grad_clip(Table<kPairs, true> t, double max_norm, const double* __restrict__ norm) {
+  const float f = clip_factor(max_norm, norm[0]);
+  const uint32_t n_chunks = t.chunks();
+  for (uint32_t c = blockIdx.x; c < n_chunks; c += gridDim.x) {
+    const int e = t.find(c), n = t.length(e, c);
+    if (f == 1.f && t.src[e].v == t.dst[e].v) continue;      // (its own output)
+    const int64_t at = t.start(e, c);
+    const bool sf = t.src[e].f32(), df = t.dst[e].f32();
+    const char* x = static_cast<const char*>(t.src[e].data()) + at * (sf ? 4 : 2);
+    char* o = static_cast<char*>(const_cast<void*>(t.dst[e].data())) + at * (df ? 4 : 2);
+    if (sf && df) scale_chunk<true, true, NT>(x, o, n, f);
+    else if (sf) scale_chunk<true, false, NT>(x, o, n, f);
+    else if (df) scale_chunk<false, true, NT>(x, o, n, f);
+    else scale_chunk<false, false, NT>(x, o, n, f);
   }
 }
 
@@ -187,7 +268,7 @@ static int check_list(const bgpo_tensor* t, int32_t count) {
     if (t[i].n < 0 || (t[i].n && !t[i].data) || (t[i].dtype != BGPO_BF16 && t[i].dtype != BGPO_F32) ||
         t[i].reserved || misaligned(t[i].data, elem_bytes(t[i])))
       return BGPO_ERR_INVALID_ARG;
-    if (t[i].n > int64_t(1) << 38) return BGPO_ERR_UNSUPPORTED;
+    if (t[i].n > int64_t(1) << 38 || (uint64_t)(uintptr_t)t[i].data >> 48) return BGPO_ERR_UNSUPPORTED;
   }
   return BGPO_OK;
 }
@@ -221,20 +302,21 @@ static int check_outputs(const bgpo_tensor* g, const bgpo_tensor* out, int32_t c
 }
 
 // Fills the table from entry `at` on; the entry it stops at.
-static int fill_table(const bgpo_tensor* g, const bgpo_tensor* out, int32_t count, int at, Table* t) {
+template <int N, bool OUT>
+static int fill_table(const bgpo_tensor* g, const bgpo_tensor* out, int32_t count, int at, Table<N, OUT>* t) {
   t->count = 0;
-  t->chunks = 0;
-  for (; at < count && t->count < kTable; ++at) {
+  uint32_t chunks = 0;
+  for (; at < count && t->count < N; ++at) {
     if (!g[at].n) continue;
+    const int64_t more = (g[at].n + kChunk - 1) / kChunk;
+    if (chunks + more > INT32_MAX) break;          // (2^24 at most for one: the first always fits)
     const int k = t->count++;
-    t->src[k] = g[at].data;
-    t->dst[k] = out ? out[at].data : nullptr;
-    t->n[k] = g[at].n;
-    t->src_f32[k] = g[at].dtype == BGPO_F32;
-    t->dst_f32[k] = out && out[at].dtype == BGPO_F32;
-    t->first[k] = t->chunks;
-    t->chunks += (uint32_t)((g[at].n + kChunk - 1) / kChunk);
+    t->src[k] = Packed::of(g[at]);
+    if (OUT) t->dst[k] = Packed::of(out[at]);
+    t->first[k] = chunks;
+    chunks += (uint32_t)more;
   }
+  t->first[t->count] = chunks;
   return at;
 }
 
@@ -242,23 +324,37 @@ template <bool MAX>
 static int run_norm(const bgpo_tensor* g, int32_t count, double* norm, int32_t* flags, double* part,
                     hipStream_t s) {
   // the workgroups that the largest launch needs take part in every one
-  Table t;
+  Table<kEntries, false> t;
   uint32_t most = 0;
+  int64_t bytes = 0;
+  for (int i = 0; i < count; ++i) bytes += g[i].n * elem_bytes(g[i]);
   for (int at = 0; at < count;) {
     at = fill_table(g, nullptr, count, at, &t);
-    most = std::max(most, t.chunks);
+    most = std::max(most, t.first[t.count]);
   }
   const int wgs = (int)std::min<uint32_t>(most, kNormWgs);
   bool first = true;
   for (int at = 0; wgs && at < count;) {
     at = fill_table(g, nullptr, count, at, &t);
     if (!t.count) break;
-    k_grad_norm<MAX><<<(unsigned)wgs, 256, 0, s>>>(t, first, part);
+    (bytes >= kStreamBytes ? k_grad_norm<MAX, true> : k_grad_norm<MAX, false>)<<<(unsigned)wgs, 256, 0, s>>>(t, first, part);
     if (hipGetLastError() != hipSuccess) return BGPO_ERR_HIP;
     first = false;
   }
   k_grad_norm_final<MAX><<<1, 256, 0, s>>>(part, wgs, norm, flags);
   return hipGetLastError() == hipSuccess ? BGPO_OK : BGPO_ERR_HIP;
+}
+
+template <int N, bool OUT, typename K>
+static int run_clip(const bgpo_tensor* g, const bgpo_tensor* out, int32_t count, K launch) {
+  Table<N, OUT> t;
+  for (int at = 0; at < count;) {
+    at = fill_table(g, out, count, at, &t);
+    if (!t.count) break;
+    launch(t, std::min<uint32_t>(t.first[t.count], kMaxClipWgs));
+    if (hipGetLastError() != hipSuccess) return BGPO_ERR_HIP;
+  }
+  return BGPO_OK;
 }
 
 }  // namespace bgpo
@@ -290,19 +386,23 @@ int bgpo_grad_clip(const bgpo_tensor* grads, const bgpo_tensor* out, int32_t cou
   if (st == BGPO_OK && out) st = check_list(out, count);
   if (st != BGPO_OK) return st;
   if (!norm || misaligned(norm, 8) || !(max_norm >= 0.0) || !isfinite(max_norm)) return BGPO_ERR_INVALID_ARG;
-  if (!out) out = grads;
-  for (int i = 0; i < count; ++i)
-    if (out[i].n != grads[i].n) return BGPO_ERR_INVALID_ARG;
-  st = check_outputs(grads, out, count);
-  if (st != BGPO_OK) return st;
-  Table t;
-  for (int at = 0; at < count;) {
-    at = fill_table(grads, out, count, at, &t);
-    if (!t.count) break;
-    k_grad_clip<<<std::min<uint32_t>(t.chunks, kMaxClipWgs), 256, 0, (hipStream_t)stream>>>(t, max_norm, norm);
-    if (hipGetLastError() != hipSuccess) return BGPO_ERR_HIP;
+  const bgpo_tensor* o = out ? out : grads;
+  int64_t bytes = 0;
+  for (int i = 0; i < count; ++i) {
+    if (o[i].n != grads[i].n) return BGPO_ERR_INVALID_ARG;
+    bytes += o[i].n * (elem_bytes(o[i]) + elem_bytes(grads[i]));
   }
-  return BGPO_OK;
+  st = check_outputs(grads, o, count);
+  if (st != BGPO_OK) return st;
+  hipStream_t s = (hipStream_t)stream;
+  const bool nt = bytes >= kStreamBytes;
+  if (out)
+    return run_clip<kPairs, true>(grads, out, count, [&](const auto& t, uint32_t wgs) {
+      (nt ? k_grad_clip<true> : k_grad_clip<false>)<<<wgs, 256, 0, s>>>(t, max_norm, norm);
+    });
+  return run_clip<kEntries, false>(grads, nullptr, count, [&](const auto& t, uint32_t wgs) {
+    (nt ? k_grad_scale<true> : k_grad_scale<false>)<<<wgs, 256, 0, s>>>(t, max_norm, norm);
+  });
 }
 
 }  // extern "C"

@@ -8,6 +8,9 @@
 // Backward: dx = scale (a (1[v = y] - p) - b p (log p + H)), element by element.
 #include <math.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "../../include/bgpo.h"
 #include "../../include/bgpo_policy.h"
 #include "common.hpp"
@@ -18,6 +21,21 @@ namespace bgpo {
 // 16 bytes of a row at any alignment the element type allows (global memory
 // takes unaligned accesses; a row of odd length starts off 16 bytes).
 typedef uint32_t raw16 __attribute__((ext_vector_type(4), aligned(2), may_alias));
+
+// Logits past the 256 MB last-level cache are streamed (nothing that is read will
+// be found there again: 4096 rows of 126464 in bf16, a fifth masked, 157 -> 138 us;
+// 70 MB took 19 and 20), gradients past the 32 MB of L2 (1009 rows of 50021: 38 -> 29).
+constexpr int64_t kStreamLogits = int64_t(256) << 20, kStreamGradient = int64_t(32) << 20;
+
+template <bool NT>
+__device__ __forceinline__ raw16 load16(const void* p) {
+  return NT ? __builtin_nontemporal_load(static_cast<const raw16*>(p)) : *static_cast<const raw16*>(p);
+}
+template <bool NT>
+__device__ __forceinline__ void store16(void* p, const raw16& v) {
+  if (NT) __builtin_nontemporal_store(v, static_cast<raw16*>(p));
+  else *static_cast<raw16*>(p) = v;
+}
 
 template <typename T>
 struct Elem;
@@ -94,12 +112,15 @@ __device__ __forceinline__ void add(RowStats& a, const float (&x)[N], float c) {
   for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
   const float ref = reference(m);
   rescale<ENT>(a, m, ref, c);
+  float s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const float u = (x[i] - ref) * c, e = __builtin_amdgcn_exp2f(u);
-    a.s += e;
-    if (ENT) a.t = fmaf(e, fmaxf(u, kNoExponent), a.t);
+    s[i & 1] += e;
+    if (ENT) t[i & 1] = fmaf(e, fmaxf(u, kNoExponent), t[i & 1]);
   }
+  a.s += s[0] + s[1];
+  if (ENT) a.t += t[0] + t[1];
 }
 
 template <bool ENT>
@@ -137,34 +158,50 @@ __device__ void finish_row(const LogitRows& p, int64_t r, int y, const RowStats&
   if (ENT) entropy[r] = ls - kLn2 * (a.t / a.s);
 }
 
-// One workgroup per row.
-template <typename T, bool ENT>
-__global__ __launch_bounds__(256) void k_logits_logp(LogitRows p, float* __restrict__ logp,
-                                                     float* __restrict__ entropy,
+// A row, or one of the n_parts pieces of `chunk` logits that a row is cut into,
+// to a workgroup: kUnroll 16-byte loads to a lane and step, whose logits share
+// one maximum.  Pieces go to `part` and are joined by k_logits_join.
+constexpr int kUnroll = 4;
+
+template <typename T, bool ENT, bool NT>
+__global__ __launch_bounds__(256) void k_logits_logp(LogitRows p, int n_parts, int chunk, RowStats* __restrict__ part,
+                                                     float* __restrict__ logp, float* __restrict__ entropy,
                                                      float* __restrict__ lse) {
   constexpr int N = Elem<T>::N;
   __shared__ RowStats red[4];
-  const int64_t r = line_index();
+  const unsigned wg = line_index();
+  const int64_t r = wg / (unsigned)n_parts;
   if (r >= p.rows) return;
   const int y = p.targets[r], tid = threadIdx.x;
   if (p.masked(r, y)) {
-    if (tid == 0) {
+    if (tid == 0 && n_parts == 1) {
       logp[r] = 0.f;
       if (lse) lse[r] = 0.f;
       if (ENT) entropy[r] = 0.f;
     }
     return;
   }
+  const int i0 = (int)(wg % (unsigned)n_parts) * chunk, end = min(p.V, i0 + chunk);
   const T* x = static_cast<const T*>(p.x) + r * p.ld;
   const float c = p.scale * kLog2e;
   RowStats a{-INFINITY, 0.f, 0.f};
-  for (int i = tid * N; i + N <= p.V; i += 256 * N) {
+  int i = i0 + tid * N;
+  for (; i + (kUnroll - 1) * 256 * N + N <= end; i += kUnroll * 256 * N) {
+    raw16 raw[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) raw[u] = load16<NT>(x + i + u * 256 * N);
+    float f[kUnroll][N];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) Elem<T>::unpack(raw[u], f[u]);
+    add<ENT>(a, reinterpret_cast<float(&)[kUnroll * N]>(f), c);
+  }
+  for (; i + N <= end; i += 256 * N) {
     float f[N];
-    Elem<T>::unpack(*reinterpret_cast<const raw16*>(x + i), f);
+    Elem<T>::unpack(load16<NT>(x + i), f);
     add<ENT>(a, f, c);
   }
-  const int i = p.V / N * N + tid;
-  if (i < p.V) {
+  i = i0 + (end - i0) / N * N + tid;
+  if (i < end) {
     const float f[1] = {Elem<T>::one(x[i])};
     add<ENT>(a, f, c);
   }
@@ -173,31 +210,59 @@ __global__ __launch_bounds__(256) void k_logits_logp(LogitRows p, float* __restr
   __syncthreads();
   if (tid) return;
   for (int w = 1; w < 4; ++w) join<ENT>(a, red[w], c);
-  finish_row<T, ENT>(p, r, y, a, logp, entropy, lse);
+  if (n_parts > 1) part[wg] = a;
+  else finish_row<T, ENT>(p, r, y, a, logp, entropy, lse);
 }
 
-// One workgroup per row.  May run in place: every element is read and written
-// by one thread.
-template <typename T>
-__global__ __launch_bounds__(256) void k_logits_logp_bwd(LogitRows p, const float* __restrict__ lse,
+// One wave per row.
+template <typename T, bool ENT>
+__global__ __launch_bounds__(256) void k_logits_join(LogitRows p, int n_parts, const RowStats* __restrict__ part,
+                                                     float* __restrict__ logp, float* __restrict__ entropy,
+                                                     float* __restrict__ lse) {
+  const int lane = threadIdx.x & 63;
+  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= p.rows) return;
+  const int y = p.targets[r];
+  if (p.masked(r, y)) {
+    if (lane == 0) {
+      logp[r] = 0.f;
+      if (lse) lse[r] = 0.f;
+      if (ENT) entropy[r] = 0.f;
+    }
+    return;
+  }
+  const float c = p.scale * kLog2e;
+  RowStats a{-INFINITY, 0.f, 0.f};
+  for (int k = lane; k < n_parts; k += 64) join<ENT>(a, part[r * n_parts + k], c);
+  a = join_wave<ENT>(a, c);
+  if (lane == 0) finish_row<T, ENT>(p, r, y, a, logp, entropy, lse);
+}
+
+// A piece of kBwdUnroll 16-byte groups to a lane.  May run in place: every element
+// is read and written by one thread.
+constexpr int kBwdUnroll = 2;
+
+template <typename T, bool ENT, bool NTL, bool NTS>
+__global__ __launch_bounds__(256) void k_logits_logp_bwd(LogitRows p, int n_parts, const float* __restrict__ lse,
                                                          const float* __restrict__ entropy,
                                                          const float* __restrict__ dlogp,
                                                          const float* __restrict__ dentropy,
                                                          T* dlogits, int64_t ld_out) {
-  constexpr int N = Elem<T>::N;
-  const int64_t r = line_index();
+  constexpr int N = Elem<T>::N, kChunk = 256 * N * kBwdUnroll;
+  const unsigned wg = line_index();
+  const int64_t r = wg / (unsigned)n_parts;
   if (r >= p.rows) return;
-  const int y = p.targets[r], tid = threadIdx.x;
+  const int y = p.targets[r], i0 = (int)(wg % (unsigned)n_parts) * kChunk;
   const T* x = static_cast<const T*>(p.x) + r * p.ld;
   T* o = dlogits + r * ld_out;
   float a = 0.f, b = 0.f, l = 0.f, h = 0.f;
   const bool masked = p.masked(r, y);
   if (!masked) {
     a = dlogp[r];
-    b = dentropy ? dentropy[r] : 0.f;
+    if (ENT) b = dentropy[r];
     l = lse[r];
     if (y >= p.V) l = NAN;
-    h = dentropy ? entropy[r] : 0.f;
+    if (ENT) h = entropy[r];
   }
   const bool none = masked || (a == 0.f && b == 0.f);
   a *= p.scale;
@@ -205,23 +270,40 @@ __global__ __launch_bounds__(256) void k_logits_logp_bwd(LogitRows p, const floa
   auto grad = [&](float v, int i) -> float {
     const float t = fmaf(v, p.scale, -l), q = __builtin_amdgcn_exp2f(t * kLog2e);
     float g = -q * a;
-    if (dentropy) g = fmaf(-q * b, fmaxf(t, kNoExponent) + h, g);
-    return i == y ? g + a : g;
+    if (ENT) g = fmaf(-q * b, fmaxf(t, kNoExponent) + h, g);
+    return g;
   };
-  for (int i = tid * N; i + N <= p.V; i += 256 * N) {
-    float f[N];
-    if (none) {
+  const int first = i0 + (int)threadIdx.x * N;
+  raw16 raw[kBwdUnroll];
 #pragma unroll
-      for (int e = 0; e < N; ++e) f[e] = 0.f;
-    } else {
-      Elem<T>::unpack(*reinterpret_cast<const raw16*>(x + i), f);
-#pragma unroll
-      for (int e = 0; e < N; ++e) f[e] = grad(f[e], i + e);
-    }
-    *reinterpret_cast<raw16*>(o + i) = Elem<T>::pack(f);
+  for (int u = 0; u < kBwdUnroll; ++u) {
+    raw[u] = (raw16){0, 0, 0, 0};
+    const int i = first + u * 256 * N;
+    if (!none && i + N <= p.V) raw[u] = load16<NTL>(x + i);
   }
-  const int i = p.V / N * N + tid;
-  if (i < p.V) o[i] = Elem<T>::round(none ? 0.f : grad(Elem<T>::one(x[i]), i));
+#pragma unroll
+  for (int u = 0; u < kBwdUnroll; ++u) {
+    const int i = first + u * 256 * N;
+    if (i + N <= p.V) {
+      float f[N];
+      if (!none) {
+        Elem<T>::unpack(raw[u], f);
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] = grad(f[e], i + e);
+        if ((unsigned)(y - i) < (unsigned)N)
+#pragma unroll
+          for (int e = 0; e < N; ++e) f[e] += i + e == y ? a : 0.f;
+        raw[u] = Elem<T>::pack(f);
+      }
+      store16<NTS>(o + i, raw[u]);
+    } else {
+      for (int k = i; k < p.V; ++k) {           // (the row's last few)
+        float g = 0.f;
+        if (!none) g = grad(Elem<T>::one(x[k]), k) + (k == y ? a : 0.f);
+        o[k] = Elem<T>::round(g);
+      }
+    }
+  }
 }
 
 static int check_logits(const bgpo_logits* p) {
@@ -231,6 +313,19 @@ static int check_logits(const bgpo_logits* p) {
   if (p->rows >= int64_t(1) << 31 || p->V > 1 << 24) return BGPO_ERR_UNSUPPORTED;
   if (bad_stride(p, p->ld, p->rows, p->V)) return BGPO_ERR_INVALID_ARG;
   return BGPO_OK;
+}
+
+// The pieces of `chunk` logits that a row is cut into: as many as give kPartWgs
+// workgroups, none below kPartElements.
+constexpr int kPartWgs = 512, kPartElements = 4096;
+struct LogitParts {
+  int n, chunk;
+};
+static LogitParts logit_parts(int64_t rows, int V) {
+  const int n = (int)std::max<int64_t>(
+      1, std::min<int64_t>((kPartWgs + rows - 1) / std::max<int64_t>(rows, 1), V / kPartElements));
+  const int chunk = ((V + n - 1) / n + 63) / 64 * 64;     // (whole 16-byte groups)
+  return LogitParts{(V + chunk - 1) / chunk, chunk};
 }
 
 static LogitRows logit_rows(const bgpo_logits* p, const void* x, const int32_t* targets,
@@ -248,7 +343,8 @@ int bgpo_logits_workspace_size(const bgpo_logits* prob, size_t* bytes) {
   const int st = check_logits(prob);
   if (st != BGPO_OK) return st;
   if (!bytes) return BGPO_ERR_INVALID_ARG;
-  *bytes = 0;
+  const int parts = logit_parts(prob->rows, prob->V).n;
+  *bytes = parts > 1 ? (size_t)prob->rows * parts * sizeof(RowStats) : 0;
   return BGPO_OK;
 }
 
@@ -267,9 +363,23 @@ int bgpo_logits_logp(const bgpo_logits* prob, const void* logits, const int32_t*
       misaligned(lse, 4) || any_overlap(out, in))
     return BGPO_ERR_INVALID_ARG;
   const LogitRows p = logit_rows(prob, logits, targets, row_mask);
-  const auto kernel = f32 ? (entropy ? k_logits_logp<float, true> : k_logits_logp<float, false>)
-                          : (entropy ? k_logits_logp<uint16_t, true> : k_logits_logp<uint16_t, false>);
-  kernel<<<line_grid(n), 256, 0, (hipStream_t)stream>>>(p, logp, entropy, lse);
+  const auto [parts, chunk] = logit_parts(n, prob->V);
+  if (parts > 1 && (!workspace || ws_bytes < (size_t)n * parts * sizeof(RowStats) || misaligned(workspace, 256)))
+    return BGPO_ERR_WORKSPACE;
+  RowStats* part = static_cast<RowStats*>(workspace);
+  hipStream_t s = (hipStream_t)stream;
+  const bool nt = n * prob->V * e > kStreamLogits;
+  const auto kernel =
+      f32 ? (entropy ? (nt ? k_logits_logp<float, true, true> : k_logits_logp<float, true, false>)
+                     : (nt ? k_logits_logp<float, false, true> : k_logits_logp<float, false, false>))
+          : (entropy ? (nt ? k_logits_logp<uint16_t, true, true> : k_logits_logp<uint16_t, true, false>)
+                     : (nt ? k_logits_logp<uint16_t, false, true> : k_logits_logp<uint16_t, false, false>));
+  kernel<<<line_grid(n * parts), 256, 0, s>>>(p, parts, chunk, part, logp, entropy, lse);
+  if (hipGetLastError() != hipSuccess) return BGPO_ERR_HIP;
+  if (parts == 1) return BGPO_OK;
+  const auto join = f32 ? (entropy ? k_logits_join<float, true> : k_logits_join<float, false>)
+                        : (entropy ? k_logits_join<uint16_t, true> : k_logits_join<uint16_t, false>);
+  join<<<(unsigned)((n + 3) / 4), 256, 0, s>>>(p, parts, part, logp, entropy, lse);
   return hipGetLastError() == hipSuccess ? BGPO_OK : BGPO_ERR_HIP;
 }
 
@@ -297,13 +407,22 @@ int bgpo_logits_logp_bwd(const bgpo_logits* prob, const void* logits, const int3
   const LogitRows p = logit_rows(prob, logits, targets, row_mask);
   const int64_t ldo = n > 1 ? ld_out : 0;
   hipStream_t s = (hipStream_t)stream;
-  if (f32)
-    k_logits_logp_bwd<float><<<line_grid(n), 256, 0, s>>>(p, lse, entropy, dlogp, dentropy,
-                                                          static_cast<float*>(dlogits), ldo);
-  else
-    k_logits_logp_bwd<uint16_t><<<line_grid(n), 256, 0, s>>>(p, lse, entropy, dlogp, dentropy,
-                                                             static_cast<uint16_t*>(dlogits), ldo);
-  return hipGetLastError() == hipSuccess ? BGPO_OK : BGPO_ERR_HIP;
+  auto launch = [&](auto kernel, auto* out) {
+    const int piece = (int)(256 * 16 / e) * kBwdUnroll, parts = (prob->V + piece - 1) / piece;
+    if (n * parts >= int64_t(1) << 32) return BGPO_ERR_UNSUPPORTED;
+    kernel<<<line_grid(n * parts), 256, 0, s>>>(p, parts, lse, entropy, dlogp, dentropy, out, ldo);
+    return hipGetLastError() == hipSuccess ? BGPO_OK : BGPO_ERR_HIP;
+  };
+  auto choose = [&](auto* out) {
+    typedef std::remove_pointer_t<decltype(out)> T;
+    const int64_t bytes = n * prob->V * e;
+    if (bytes > kStreamLogits)
+      return dentropy ? launch(k_logits_logp_bwd<T, true, true, true>, out) : launch(k_logits_logp_bwd<T, false, true, true>, out);
+    if (bytes > kStreamGradient)
+      return dentropy ? launch(k_logits_logp_bwd<T, true, false, true>, out) : launch(k_logits_logp_bwd<T, false, false, true>, out);
+    return dentropy ? launch(k_logits_logp_bwd<T, true, false, false>, out) : launch(k_logits_logp_bwd<T, false, false, false>, out);
+  };
+  return f32 ? choose(static_cast<float*>(dlogits)) : choose(static_cast<uint16_t*>(dlogits));
 }
 
 }  // extern "C"

@@ -240,7 +240,7 @@ def _list(b, *entries):
 
 BAD_ENTRIES = [((1 << 44, -1, 1, 0), INVALID), ((None, 4, 1, 0), INVALID), ((1 << 44, 4, 2, 0), INVALID),
                ((1 << 44, 4, -1, 0), INVALID), ((1 << 44, 4, 1, 1), INVALID), (((1 << 44) + 2, 4, 1, 0), INVALID),
-               (((1 << 44) + 1, 4, 0, 0), INVALID), ((1 << 44, (1 << 38) + 1, 1, 0), UNSUPPORTED)]
+               (((1 << 44) + 1, 4, 0, 0), INVALID), ((1 << 44, (1 << 38) + 1, 1, 0), UNSUPPORTED), ((1 << 48, 4, 1, 0), UNSUPPORTED)]
 
 
 @pytest.mark.parametrize("entry,status", BAD_ENTRIES)
@@ -274,7 +274,7 @@ def test_gradient_arguments(b):
     assert clip(g, None, 2, 1.0, ctypes.c_void_p(at(3).value + 4), None) == INVALID
     assert clip(None, None, 0, 1.0, at(3), None) == 0                    # nothing to do
     # outputs of another size, twice the same tensor, outputs over other entries
-    assert clip(g, _list(b, (1 << 47, 8, 1, 0), (1 << 48, 7, 0, 0)), 2, 1.0, at(3), None) == INVALID
+    assert clip(g, _list(b, (1 << 47, 8, 1, 0), ((1 << 47) + (1 << 40), 7, 0, 0)), 2, 1.0, at(3), None) == INVALID
     a = 1 << 45
     for entries in ([(a, 8, 1, 0), (a, 8, 1, 0)], [(a, 8, 1, 0), (a + 28, 8, 1, 0)], [(a + 28, 8, 0, 0), (a, 8, 1, 0)]):
         assert clip(_list(b, *entries), None, 2, 1.0, at(3), None) == INVALID
