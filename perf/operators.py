@@ -266,6 +266,12 @@ def prepare(case, seed):
 
 # ---------------------------------------------------------------- the framework's calls
 
+def _own_scale(c):
+    """The scale as the plain form weighs with it: a sum's is a number of 32 bits there."""
+    scale = _policy_scale(c)
+    return float(torch.tensor(scale, dtype=torch.float32)) if c["reduce"] == "sum" else scale
+
+
 def _own(s):
     from paper_2510_11683_amd import bgpo
     if s["op"] == "logp":
@@ -283,7 +289,7 @@ def _own(s):
         if "ws" not in s:
             s["prob"] = bgpo.PolicyLoss(c["B"], c["L"], ratio=RATIO[c["ratio"]], reduce=REDUCE[c["reduce"]], kl=KL[c["kl"]],
                                         clip_low=c["clip_low"], clip_high=c["clip_high"], clip_dual=c["clip_dual"],
-                                        kl_coef=c["kl_coef"], loss_scale=_policy_scale(c))
+                                        kl_coef=c["kl_coef"], loss_scale=_own_scale(c))
             s["ws"] = bgpo.policy_workspace(s["prob"])
         bgpo.bgpo_policy_loss(s["prob"], s["logp"], s["old"], s["ref"], s["adv"], s["mask"], s["dlogp"], s["stats"], s["ws"])
         return [s["stats"][:4], s["stats"][4:], s["dlogp"]]
