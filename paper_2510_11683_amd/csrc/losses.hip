@@ -457,37 +457,53 @@ __device__ __forceinline__ T position_loss(const PolicyArgs& p, const PolicyRow&
   return g;
 }
 
+// What a lane of a short row holds: its positions and their values.
+template <typename T, int G, bool TOKEN, int KL>
+struct ShortTile {
+  static constexpr int U = 4;
+  Positions<G, U> k;
+  T x[U], o[U], q[U];
+  float A[U];
+
+  // the mask first; then the arrays (`sums`: what a sequence ratio's sum needs too)
+  __device__ __forceinline__ void load_values(const PolicyArgs& p, int b, int i, bool sums) {
+    if (TOKEN || KL || sums) k.values(static_cast<const T*>(p.logp) + b * p.ld_logp, i, x);
+    if ((TOKEN || sums) && p.old) k.values(static_cast<const T*>(p.old) + b * p.ld_old, i, o);
+    if (KL) k.values(static_cast<const T*>(p.ref) + b * p.ld_ref, i, q);
+    if (TOKEN && p.ld_adv) k.values(p.adv + b * p.ld_adv, i, A);
+  }
+  __device__ __forceinline__ double log_ratio() const {
+    double d = 0.0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) d += k.live[u] ? (double)x[u] - (double)o[u] : 0.0;
+    return d;
+  }
+  __device__ __forceinline__ void loss(const PolicyArgs& p, const PolicyRow& row, PolicySums& s, T& bad, T (&g)[U]) const {
+    s.positions += k.count();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      g[u] = position_loss<TOKEN, KL>(p, row, k.live[u], x[u], o[u], q[u], p.ld_adv ? (double)A[u] : row.A, s, bad);
+      if (u % 2) __builtin_amdgcn_sched_barrier(0);   // (two exponentials at a time: more take registers)
+    }
+  }
+};
+
 // Objective and gradient of [i0, end) of a response.
 template <typename T, int G, bool TOKEN, int KL>
 __device__ __forceinline__ void row_loss(const PolicyArgs& p, const PolicyRow& row, int b, int i0, int end, PolicySums& s,
                                          T& bad) {
-  constexpr int U = 4;
-  const uint8_t* mask = p.mask + b * p.ld_mask;
-  const T* logp = static_cast<const T*>(p.logp) + b * p.ld_logp;
-  const T* old = static_cast<const T*>(p.old) + b * p.ld_old;
-  const T* ref = static_cast<const T*>(p.ref) + b * p.ld_ref;
-  const float* adv = p.adv + b * p.ld_adv;
+  typedef ShortTile<T, G, TOKEN, KL> Tile;
   T* dlogp = static_cast<T*>(p.dlogp) + b * p.ld_dlogp;
-  for (int j = i0; j < end; j += G * U) {
+  for (int j = i0; j < end; j += G * Tile::U) {
     const int i = j + (int)(threadIdx.x % G);
-    Positions<G, U> k;
-    k.load(mask, i, end);
-    T g[U] = {0, 0, 0, 0};
-    if (k.any()) {
-      T x[U] = {0, 0, 0, 0}, o[U] = {0, 0, 0, 0}, q[U] = {0, 0, 0, 0};
-      float A[U];
-      if (TOKEN || KL) k.values(logp, i, x);
-      if (TOKEN && p.old) k.values(old, i, o);
-      if (KL) k.values(ref, i, q);
-      if (TOKEN && p.ld_adv) k.values(adv, i, A);
-      s.positions += k.count();
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        g[u] = position_loss<TOKEN, KL>(p, row, k.live[u], x[u], o[u], q[u], p.ld_adv ? (double)A[u] : row.A, s, bad);
-        if (u % 2) __builtin_amdgcn_sched_barrier(0);   // (two exponentials at a time: more take registers)
-      }
+    Tile t;
+    t.k.load(p.mask + b * p.ld_mask, i, end);
+    T g[Tile::U] = {0, 0, 0, 0};
+    if (t.k.any()) {
+      t.load_values(p, b, i, false);
+      t.loss(p, row, s, bad, g);
     }
-    if (p.dlogp) k.store(dlogp, i, end, g);
+    if (p.dlogp) t.k.store(dlogp, i, end, g);
   }
 }
 
@@ -737,24 +753,58 @@ __global__ __launch_bounds__(kStatsThreads) void k_policy_stats(PolicyArgs p, in
 }
 
 // A small batch in one launch of one workgroup: the passes above with barriers
-// between them, pieces of four positions to a lane.
+// between them, or, where no group has more than one tile of one piece, with
+// everything read at once and kept.
 constexpr int kSmallThreads = 1024;
 
-template <typename T, int G, bool TOKEN, int KL>
+template <typename T, int G, bool TOKEN, int KL, bool TILE>
 __global__ __launch_bounds__(kSmallThreads) void k_policy_small(PolicyArgs p) {
   constexpr int kGroups = kSmallThreads / G;
   __shared__ double red[kSmallThreads / 64][kPolicySums];
-  const int group = group_index<G, kSmallThreads>();
+  const int group = group_index<G, kSmallThreads>(), lane = threadIdx.x % G;
   double w = p.loss_scale;
-  if (p.rows) {
-    double n[1] = {rows_pass<T, G, TOKEN>(p, group, kGroups, nullptr)};
-    if (threadIdx.x % G) n[0] = 0.0;
-    group_sum<kSmallThreads, 1>(n, reinterpret_cast<double(*)[1]>(red));   // (its barriers publish p.rows)
-    if (p.reduce == BGPO_REDUCE_TOKENS) w = n[0] > 0.0 ? p.loss_scale / n[0] : 0.0;
-  }
   double sums[kPolicySums] = {0.0, 0.0, 0.0, 0.0, 0.0};
   T bad = 0;
-  loss_pass<T, G, TOKEN, KL>(p, group, kGroups, w, sums, bad, nullptr);
+  if constexpr (TILE) {
+    __shared__ double2 rows[kGroups];
+    typedef ShortTile<T, G, TOKEN, KL> Tile;
+    const bool mine = (uint32_t)group < p.pieces();
+    const int b = mine ? group / p.n_chunks : 0, i0 = mine ? group % p.n_chunks * p.chunk : 0;
+    const int i = i0 + lane, end = mine ? min(p.L, i0 + p.chunk) : 0;
+    Tile t;
+    t.k.load(p.mask + b * p.ld_mask, i, end);
+    t.load_values(p, b, i, p.ratio == BGPO_RATIO_SEQUENCE);
+    {
+      double v[2] = {(double)t.k.count(), !TOKEN && p.old ? t.log_ratio() : 0.0}, n[1] = {v[0]};
+      group_sum<G, 2>(v, nullptr);
+      if (lane == 0) rows[group] = make_double2(v[0], v[1]);
+      group_sum<kSmallThreads, 1>(n, reinterpret_cast<double(*)[1]>(red));   // (its barriers publish rows)
+      if (p.reduce == BGPO_REDUCE_TOKENS) w = n[0] > 0.0 ? p.loss_scale / n[0] : 0.0;
+    }
+    if (mine) {
+      double2 v = make_double2(0.0, 0.0);
+      if (p.whole_rows())
+        for (int c = 0; c < p.n_chunks; ++c) {
+          v.x += rows[b * p.n_chunks + c].x;
+          v.y += rows[b * p.n_chunks + c].y;
+        }
+      const PolicyRow row = policy_row<G, TOKEN>(p, b, w, v.x, v.y);
+      PolicySums s;
+      if (!TOKEN && lane == 0 && i0 == 0) s.d = v.y;
+      T g[Tile::U];
+      t.loss(p, row, s, bad, g);
+      if (p.dlogp) t.k.store(static_cast<T*>(p.dlogp) + b * p.ld_dlogp, i, end, g);
+      add_sums<TOKEN>(row, s, sums);
+    }
+  } else {
+    if (p.rows) {
+      double n[1] = {rows_pass<T, G, TOKEN>(p, group, kGroups, nullptr)};
+      if (lane) n[0] = 0.0;
+      group_sum<kSmallThreads, 1>(n, reinterpret_cast<double(*)[1]>(red));   // (its barriers publish p.rows)
+      if (p.reduce == BGPO_REDUCE_TOKENS) w = n[0] > 0.0 ? p.loss_scale / n[0] : 0.0;
+    }
+    loss_pass<T, G, TOKEN, KL>(p, group, kGroups, w, sums, bad, nullptr);
+  }
   if (bad != bad && p.dlogp && p.flags) atomicOr(p.flags, kFlagNonfinite);
   group_sum<kSmallThreads, kPolicySums>(sums, red);
   if (threadIdx.x == 0) write_policy_stats(p, sums);
@@ -831,8 +881,12 @@ static int launch_policy(PolicyArgs p, const PolicyPlan& q, hipStream_t s) {
 template <typename T, bool TOKEN, int KL>
 static int run_policy(const PolicyArgs& p, const PolicyPlan& q, hipStream_t s) {
   if (q.small) {
-    if (q.lanes == 16) k_policy_small<T, 16, TOKEN, KL><<<1, kSmallThreads, 0, s>>>(p);
-    else k_policy_small<T, 64, TOKEN, KL><<<1, kSmallThreads, 0, s>>>(p);
+    // (8 x 512: 11.3 -> 9.5 us; without sums over the whole batch there is no barrier
+    // to read ahead of: 16 x 32 samples 6.5 us, 8.3 kept)
+    const bool tile = q.rows_pass && q.pieces <= kSmallThreads / q.lanes && q.chunk <= q.lanes * 4;
+    const auto kernel = q.lanes == 16 ? (tile ? k_policy_small<T, 16, TOKEN, KL, true> : k_policy_small<T, 16, TOKEN, KL, false>)
+                                      : (tile ? k_policy_small<T, 64, TOKEN, KL, true> : k_policy_small<T, 64, TOKEN, KL, false>);
+    kernel<<<1, kSmallThreads, 0, s>>>(p);
     return hipGetLastError() == hipSuccess ? BGPO_OK : BGPO_ERR_HIP;
   }
   switch (q.lanes) {

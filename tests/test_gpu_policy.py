@@ -332,3 +332,55 @@ def test_calls_are_deterministic_and_replay():
                     torch.cuda.synchronize()
                     got.append([t.clone() for t in outs])
                 assert all(torch.equal(p, q) for o in got[1:] for p, q in zip(got[0], o))
+
+
+def test_exponentials_over_their_range():
+    """The kernels' own e^x and e^x - 1 through the loss's gradient (fp64, one
+    position to a weight of 1).  The series leaves 2^-50.8 |f| <= 1.1 2^-52 of e^f, its
+    Horner steps and the final sum about 2.5 more: 6 2^-52 of e^x; of e^x - 1 that is up
+    to 3.4 times as much where 2^n first differs from 1 (|x| near 0.35)."""
+    rng = np.random.default_rng(9)
+    x = np.concatenate([np.linspace(-760, 712, 4001), rng.uniform(-1, 1, 3000), 10.0 ** rng.uniform(-18, 0, 2000),
+                        -10.0 ** rng.uniform(-18, 0, 2000), [0.0, 709.78, 709.79, -745.1, -745.2, -np.inf, np.inf]])
+    for L in (len(x), 512):                                  # the long rows' kernel and the small batch's
+        v = x[:L] if L < len(x) else x
+        z, one, on = np.zeros((1, len(v))), np.ones(1, np.float32), np.ones((1, len(v)), np.uint8)
+        _, g = _run_policy(v[None].copy(), z, None, one, on, torch.float64, reduce="sum", clip_low=1.0, clip_high=math.inf)
+        with np.errstate(over="ignore"):
+            want = np.exp(v)
+        fin = np.isfinite(want)
+        assert np.array_equal(-g[0][~fin], want[~fin])
+        assert (np.abs(-g[0][fin] - want[fin]) <= 6 * E52 * want[fin] + 2.0 ** -1073).all()
+        # q = ref - logp, no policy term: d KL / d logp = -(e^q - 1)
+        _, g = _run_policy(z.copy(), None, v[None].copy(), 0 * one, on, torch.float64, reduce="sum", kl="k3", kl_coef=1.0)
+        with np.errstate(over="ignore"):
+            want = np.expm1(v)
+        assert np.array_equal(-g[0][~fin], want[~fin])
+        assert (np.abs(-g[0][fin] - want[fin]) <= 20 * E52 * np.abs(want[fin]) + 2.0 ** -1073).all()
+
+
+@pytest.mark.parametrize("where", ["prompt", "gap", "one", "last"])
+def test_long_rows_by_where_they_count(where):
+    """Masks whose live range starts late, has a gap, is one position, or ends with
+    the row; lengths about every step of the long rows' kernel."""
+    for L in (513, 516, 1023, 1024, 1025, 2050, 4099):
+        lp, old, ref, adv, mask = _policy_inputs(3, L, torch.float32, seed=7, empty=False)
+        lp, old, ref = (np.nan_to_num(v, nan=-1.0) for v in (lp, old, ref))
+        mask[:] = 0
+        if where == "prompt":
+            mask[0, L // 3:], mask[1, L // 2: L - 5], mask[2, 1:] = 1, 1, 1
+        elif where == "gap":
+            mask[0, :7], mask[0, L - 9:], mask[1, 255:258], mask[2, ::97] = 1, 1, 1, 1
+        elif where == "one":
+            mask[0, 0], mask[1, L - 1], mask[2, L // 2] = 1, 1, 1
+        else:
+            mask[0, L - 1], mask[1, L - 4:], mask[2, L - 6: L - 1] = 1, 1, 1
+        for a in (lp, old, ref):
+            a[mask == 0] = np.nan
+        for ratio, reduce in itertools.product(RATIO, REDUCE):
+            _check_policy(lp, old, ref, adv, mask, torch.float32, pad=1, ratio=ratio, reduce=reduce, clip_low=0.1, kl_coef=0.1)
+        a = dict(win=lp, lose=old, win_ref=ref, lose_ref=ref, win_mask=mask, lose_mask=np.roll(mask, 1, 0))
+        for k in ("lose", "lose_ref"):
+            a[k] = np.where(a["lose_mask"] == 0, np.float32(np.nan), np.nan_to_num(a[k], nan=-1.5)).astype(np.float32)
+        for mean in (False, True):
+            _check_pref(a, torch.float32, pad=1, kind="sigmoid", mean=mean)
