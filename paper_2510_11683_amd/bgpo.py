@@ -82,11 +82,12 @@ class _Preference(ctypes.Structure):
                 [(k, ctypes.c_int32) for k in ("P", "L", "dtype", "kind", "mean", "reserved")])
 
 
-# the same structures as bytes (passed as they are: a third of the time that a
-# ctypes structure takes to build)
+# the same structures as bytes (built in a third of the time that a ctypes
+# structure takes)
+_LOGITS = struct.Struct("2q2ifi")
 _POLICY = struct.Struct("6q5d6i")
 _PREFERENCE = struct.Struct("9q4d6i")
-assert _POLICY.size == ctypes.sizeof(_Policy) and _PREFERENCE.size == ctypes.sizeof(_Preference)
+assert _LOGITS.size == ctypes.sizeof(_Logits) and _POLICY.size == ctypes.sizeof(_Policy) and _PREFERENCE.size == ctypes.sizeof(_Preference)
 
 
 class Timing(ctypes.Structure):
@@ -128,8 +129,8 @@ def _load():
     lib.bgpo_moments_workspace_size.argtypes = []
     lib.bgpo_moments_summary.argtypes = [vp, vp, vp, ctypes.c_int64, i32, vp, vp, sz, vp]
     lib.bgpo_logits_workspace_size.argtypes = [P(_Logits), P(sz)]
-    lib.bgpo_logits_logp.argtypes = [P(_Logits), vp, vp, vp, vp, vp, vp, vp, sz, vp]
-    lib.bgpo_logits_logp_bwd.argtypes = [P(_Logits), vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_int64, vp]
+    lib.bgpo_logits_logp.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.bgpo_logits_logp_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_int64, vp]
     lib.bgpo_policy_workspace_size.argtypes = [P(_Policy), P(sz)]
     lib.bgpo_policy_loss.argtypes = [vp] * 10 + [sz, vp]
     lib.bgpo_preference_workspace_size.argtypes = [P(_Preference), P(sz)]
@@ -496,14 +497,12 @@ def _workspace_args(ws: Optional[torch.Tensor], device: int):
 
 
 def _logits_problem(logits, scale: float, device: int):
+    """(the bgpo_logits, address, rows, V)"""
     if logits.dim() != 2:
         raise ValueError("logits must be a matrix [rows, V]")
     rows, V = logits.shape
-    if rows == 0 or V == 0:
-        ld = V
-    else:
-        _, ld = _mat(logits, "logits", (torch.bfloat16, torch.float32), rows, V, device)
-    return _Logits(rows, ld, V, BGPO_F32 if logits.dtype == torch.float32 else BGPO_BF16, scale, 0)
+    at, ld = (None, V) if rows == 0 else _mat(logits, "logits", (torch.bfloat16, torch.float32), rows, V, device)
+    return _LOGITS.pack(rows, ld, V, BGPO_F32 if logits.dtype == torch.float32 else BGPO_BF16, scale, 0), at, rows, V
 
 
 def bgpo_logits_workspace_size(rows: int, V: int) -> int:
@@ -522,11 +521,10 @@ def bgpo_logits_logp(logits, targets, logp, entropy=None, lse=None, workspace=No
                      stream=None):
     """Log-probability of each row's target (and the entropy and log-sum-exp)."""
     dev = _device(logits)
-    prob = _logits_problem(logits, scale, dev)
-    n = prob.rows
+    prob, at, n, _ = _logits_problem(logits, scale, dev)
     ws, ws_bytes = _workspace_args(workspace, dev)
     _check(_lib.bgpo_logits_logp(
-        ctypes.byref(prob), logits.data_ptr(), _vec(targets, "targets", (torch.int32,), n, dev),
+        prob, at, _vec(targets, "targets", (torch.int32,), n, dev),
         _vec(row_mask, "row_mask", _U8, n, dev, allow_none=True), _vec(logp, "logp", _F32, n, dev),
         _vec(entropy, "entropy", _F32, n, dev, allow_none=True), _vec(lse, "lse", _F32, n, dev, allow_none=True),
         ws, ws_bytes, _stream(stream)), "bgpo_logits_logp")
@@ -537,11 +535,10 @@ def bgpo_logits_logp_bwd(logits, targets, lse, entropy, dlogp, dentropy, dlogits
     """Gradient of the logits from those of logp and the entropy; dlogits may be
     logits itself."""
     dev = _device(logits)
-    prob = _logits_problem(logits, scale, dev)
-    n = prob.rows
-    out, ld_out = _mat(dlogits, "dlogits", (logits.dtype,), n, prob.V, dev)
+    prob, at, n, V = _logits_problem(logits, scale, dev)
+    out, ld_out = _mat(dlogits, "dlogits", (logits.dtype,), n, V, dev)
     _check(_lib.bgpo_logits_logp_bwd(
-        ctypes.byref(prob), logits.data_ptr(), _vec(targets, "targets", (torch.int32,), n, dev),
+        prob, at, _vec(targets, "targets", (torch.int32,), n, dev),
         _vec(row_mask, "row_mask", _U8, n, dev, allow_none=True), _vec(lse, "lse", _F32, n, dev),
         _vec(entropy, "entropy", _F32, n, dev, allow_none=True), _vec(dlogp, "dlogp", _F32, n, dev),
         _vec(dentropy, "dentropy", _F32, n, dev, allow_none=True), out, ld_out, _stream(stream)),
@@ -685,6 +682,7 @@ class GradList:
                 _refuse(t, f"gradient {i}", (torch.bfloat16, torch.float32), tuple(t.shape), _device(t))
             if not t.is_contiguous():
                 raise ValueError(f"gradient {i} must be contiguous")
+        self._device = _device(self.tensors[0]) if self.tensors else None
         self._at = self._where()
         # (kept, so that an address seen again is the same memory)
         self._storage = [t.untyped_storage() for t in self.tensors]
@@ -698,9 +696,11 @@ class GradList:
     def _where(self):
         return list(map(torch.Tensor.data_ptr, self.tensors))
 
-    def c(self):
+    def c(self, device: int):
         if self._at != self._where():
             self.__init__(self.tensors)
+        if self.tensors and self._device != device:
+            raise ValueError("the gradients are on another device than the current one")
         return self._c
 
 
@@ -713,7 +713,7 @@ def bgpo_grad_norm(grads: GradList, norm, workspace, norm_type: int = BGPO_NORM_
     """norm[0] = the norm of all gradients of the list as one vector."""
     dev = _device(norm)
     ws, ws_bytes = _workspace_args(workspace, dev)
-    _check(_lib.bgpo_grad_norm(grads.c(), len(grads), norm_type, _vec(norm, "norm", (torch.float64,), 1, dev),
+    _check(_lib.bgpo_grad_norm(grads.c(dev), len(grads), norm_type, _vec(norm, "norm", (torch.float64,), 1, dev),
                                _vec(status_flags, "status_flags", (torch.int32,), 1, dev, allow_none=True), ws, ws_bytes,
                                _stream(stream)), "bgpo_grad_norm")
 
@@ -724,7 +724,7 @@ def bgpo_grad_clip(grads: GradList, max_norm: float, norm, out: Optional[GradLis
     if out is not None and len(out) != len(grads):
         raise ValueError(f"out has {len(out)} tensors, expected {len(grads)}")
     dev = _device(norm)
-    _check(_lib.bgpo_grad_clip(grads.c(), None if out is None else out.c(), len(grads), float(max_norm),
+    _check(_lib.bgpo_grad_clip(grads.c(dev), None if out is None else out.c(dev), len(grads), float(max_norm),
                                _vec(norm, "norm", (torch.float64,), 1, dev), _stream(stream)), "bgpo_grad_clip")
 
 

@@ -159,58 +159,64 @@ __device__ void finish_row(const LogitRows& p, int64_t r, int y, const RowStats&
 }
 
 // A row, or one of the n_parts pieces of `chunk` logits that a row is cut into,
-// to a workgroup: kUnroll 16-byte loads to a lane and step, whose logits share
-// one maximum.  Pieces go to `part` and are joined by k_logits_join.
+// to a workgroup (LANES 256) or a wave (64): kUnroll 16-byte loads to a lane and
+// step, whose logits share one maximum.  Pieces go to `part` and are joined by
+// k_logits_join.  Bound by HBM: 4096 rows of 126464 in bf16, a fifth masked, with
+// entropies 138 us (6.0 TB/s), of which its vector work (8 instructions to a logit,
+// 32 cycles of a wave) would take 60 %.
 constexpr int kUnroll = 4;
 
-template <typename T, bool ENT, bool NT>
+template <typename T, bool ENT, bool NT, int LANES>
 __global__ __launch_bounds__(256) void k_logits_logp(LogitRows p, int n_parts, int chunk, RowStats* __restrict__ part,
                                                      float* __restrict__ logp, float* __restrict__ entropy,
                                                      float* __restrict__ lse) {
   constexpr int N = Elem<T>::N;
   __shared__ RowStats red[4];
-  const unsigned wg = line_index();
-  const int64_t r = wg / (unsigned)n_parts;
+  const unsigned item = LANES == 256 ? line_index() : line_index() * 4 + (threadIdx.x >> 6);
+  const int64_t r = item / (unsigned)n_parts;
   if (r >= p.rows) return;
-  const int y = p.targets[r], tid = threadIdx.x;
+  const int y = p.targets[r], lane = threadIdx.x % LANES;
   if (p.masked(r, y)) {
-    if (tid == 0 && n_parts == 1) {
+    if (lane == 0 && n_parts == 1) {
       logp[r] = 0.f;
       if (lse) lse[r] = 0.f;
       if (ENT) entropy[r] = 0.f;
     }
     return;
   }
-  const int i0 = (int)(wg % (unsigned)n_parts) * chunk, end = min(p.V, i0 + chunk);
+  const int i0 = (int)(item % (unsigned)n_parts) * chunk, end = min(p.V, i0 + chunk);
   const T* x = static_cast<const T*>(p.x) + r * p.ld;
   const float c = p.scale * kLog2e;
   RowStats a{-INFINITY, 0.f, 0.f};
-  int i = i0 + tid * N;
-  for (; i + (kUnroll - 1) * 256 * N + N <= end; i += kUnroll * 256 * N) {
+  int i = i0 + lane * N;
+  for (; i + (kUnroll - 1) * LANES * N + N <= end; i += kUnroll * LANES * N) {
     raw16 raw[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) raw[u] = load16<NT>(x + i + u * 256 * N);
+    for (int u = 0; u < kUnroll; ++u) raw[u] = load16<NT>(x + i + u * LANES * N);
     float f[kUnroll][N];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) Elem<T>::unpack(raw[u], f[u]);
     add<ENT>(a, reinterpret_cast<float(&)[kUnroll * N]>(f), c);
   }
-  for (; i + N <= end; i += 256 * N) {
+  for (; i + N <= end; i += LANES * N) {
     float f[N];
     Elem<T>::unpack(load16<NT>(x + i), f);
     add<ENT>(a, f, c);
   }
-  i = i0 + (end - i0) / N * N + tid;
+  i = i0 + (end - i0) / N * N + lane;
   if (i < end) {
     const float f[1] = {Elem<T>::one(x[i])};
     add<ENT>(a, f, c);
   }
   a = join_wave<ENT>(a, c);
-  if ((tid & 63) == 0) red[tid >> 6] = a;
-  __syncthreads();
-  if (tid) return;
-  for (int w = 1; w < 4; ++w) join<ENT>(a, red[w], c);
-  if (n_parts > 1) part[wg] = a;
+  if constexpr (LANES == 256) {
+    if ((lane & 63) == 0) red[lane >> 6] = a;
+    __syncthreads();
+    if (lane) return;
+    for (int w = 1; w < 4; ++w) join<ENT>(a, red[w], c);
+  }
+  if (lane) return;
+  if (n_parts > 1) part[item] = a;
   else finish_row<T, ENT>(p, r, y, a, logp, entropy, lse);
 }
 
@@ -238,21 +244,23 @@ __global__ __launch_bounds__(256) void k_logits_join(LogitRows p, int n_parts, c
   if (lane == 0) finish_row<T, ENT>(p, r, y, a, logp, entropy, lse);
 }
 
-// A piece of kBwdUnroll 16-byte groups to a lane.  May run in place: every element
-// is read and written by one thread.
+// A piece of kBwdUnroll 16-byte groups to a lane, of a workgroup or a wave.  May
+// run in place: every element is read and written by one thread.  Bound by HBM: 4096
+// rows of 126464 in bf16, a fifth masked, 288 us (6.2 TB/s; one group to a lane 308,
+// four 310, eight 552).
 constexpr int kBwdUnroll = 2;
 
-template <typename T, bool ENT, bool NTL, bool NTS>
+template <typename T, bool ENT, bool NTL, bool NTS, int LANES>
 __global__ __launch_bounds__(256) void k_logits_logp_bwd(LogitRows p, int n_parts, const float* __restrict__ lse,
                                                          const float* __restrict__ entropy,
                                                          const float* __restrict__ dlogp,
                                                          const float* __restrict__ dentropy,
                                                          T* dlogits, int64_t ld_out) {
-  constexpr int N = Elem<T>::N, kChunk = 256 * N * kBwdUnroll;
-  const unsigned wg = line_index();
-  const int64_t r = wg / (unsigned)n_parts;
+  constexpr int N = Elem<T>::N, kChunk = LANES * N * kBwdUnroll;
+  const unsigned item = LANES == 256 ? line_index() : line_index() * 4 + (threadIdx.x >> 6);
+  const int64_t r = item / (unsigned)n_parts;
   if (r >= p.rows) return;
-  const int y = p.targets[r], i0 = (int)(wg % (unsigned)n_parts) * kChunk;
+  const int y = p.targets[r], i0 = (int)(item % (unsigned)n_parts) * kChunk;
   const T* x = static_cast<const T*>(p.x) + r * p.ld;
   T* o = dlogits + r * ld_out;
   float a = 0.f, b = 0.f, l = 0.f, h = 0.f;
@@ -273,17 +281,17 @@ __global__ __launch_bounds__(256) void k_logits_logp_bwd(LogitRows p, int n_part
     if (ENT) g = fmaf(-q * b, fmaxf(t, kNoExponent) + h, g);
     return g;
   };
-  const int first = i0 + (int)threadIdx.x * N;
+  const int first = i0 + (int)(threadIdx.x % LANES) * N;
   raw16 raw[kBwdUnroll];
 #pragma unroll
   for (int u = 0; u < kBwdUnroll; ++u) {
     raw[u] = (raw16){0, 0, 0, 0};
-    const int i = first + u * 256 * N;
+    const int i = first + u * LANES * N;
     if (!none && i + N <= p.V) raw[u] = load16<NTL>(x + i);
   }
 #pragma unroll
   for (int u = 0; u < kBwdUnroll; ++u) {
-    const int i = first + u * 256 * N;
+    const int i = first + u * LANES * N;
     if (i + N <= p.V) {
       float f[N];
       if (!none) {
@@ -316,8 +324,12 @@ static int check_logits(const bgpo_logits* p) {
 }
 
 // The pieces of `chunk` logits that a row is cut into: as many as give kPartWgs
-// workgroups, none below kPartElements.
+// workgroups, none below kPartElements (8 rows of 126464 in bf16: 17.2 -> 10.9 us; 777
+// rows of 32003 in fp32, cut into 3, took 19.0, whole 15.9).
 constexpr int kPartWgs = 512, kPartElements = 4096;
+// Rows of up to this many logits are a wave's work each (8192 rows of 3001 in bf16:
+// 16.6 us with a workgroup each, 12.1 so).
+constexpr int kWaveElements = 4096;
 struct LogitParts {
   int n, chunk;
 };
@@ -368,13 +380,20 @@ int bgpo_logits_logp(const bgpo_logits* prob, const void* logits, const int32_t*
     return BGPO_ERR_WORKSPACE;
   RowStats* part = static_cast<RowStats*>(workspace);
   hipStream_t s = (hipStream_t)stream;
-  const bool nt = n * prob->V * e > kStreamLogits;
-  const auto kernel =
-      f32 ? (entropy ? (nt ? k_logits_logp<float, true, true> : k_logits_logp<float, true, false>)
-                     : (nt ? k_logits_logp<float, false, true> : k_logits_logp<float, false, false>))
-          : (entropy ? (nt ? k_logits_logp<uint16_t, true, true> : k_logits_logp<uint16_t, true, false>)
-                     : (nt ? k_logits_logp<uint16_t, false, true> : k_logits_logp<uint16_t, false, false>));
-  kernel<<<line_grid(n * parts), 256, 0, s>>>(p, parts, chunk, part, logp, entropy, lse);
+  auto launch = [&](auto wave, auto workgroup) {
+    if (prob->V <= kWaveElements) wave<<<line_grid((n + 3) / 4), 256, 0, s>>>(p, 1, chunk, part, logp, entropy, lse);
+    else workgroup<<<line_grid(n * parts), 256, 0, s>>>(p, parts, chunk, part, logp, entropy, lse);
+  };
+  auto choose = [&](auto* x) {
+    typedef std::remove_pointer_t<decltype(x)> T;
+    const bool nt = n * prob->V * e > kStreamLogits;
+    if (entropy && nt) launch(k_logits_logp<T, true, true, 64>, k_logits_logp<T, true, true, 256>);
+    else if (entropy) launch(k_logits_logp<T, true, false, 64>, k_logits_logp<T, true, false, 256>);
+    else if (nt) launch(k_logits_logp<T, false, true, 64>, k_logits_logp<T, false, true, 256>);
+    else launch(k_logits_logp<T, false, false, 64>, k_logits_logp<T, false, false, 256>);
+  };
+  if (f32) choose(static_cast<float*>(nullptr));
+  else choose(static_cast<uint16_t*>(nullptr));
   if (hipGetLastError() != hipSuccess) return BGPO_ERR_HIP;
   if (parts == 1) return BGPO_OK;
   const auto join = f32 ? (entropy ? k_logits_join<float, true> : k_logits_join<float, false>)
@@ -407,20 +426,25 @@ int bgpo_logits_logp_bwd(const bgpo_logits* prob, const void* logits, const int3
   const LogitRows p = logit_rows(prob, logits, targets, row_mask);
   const int64_t ldo = n > 1 ? ld_out : 0;
   hipStream_t s = (hipStream_t)stream;
-  auto launch = [&](auto kernel, auto* out) {
-    const int piece = (int)(256 * 16 / e) * kBwdUnroll, parts = (prob->V + piece - 1) / piece;
-    if (n * parts >= int64_t(1) << 32) return BGPO_ERR_UNSUPPORTED;
-    kernel<<<line_grid(n * parts), 256, 0, s>>>(p, parts, lse, entropy, dlogp, dentropy, out, ldo);
+  auto launch = [&](auto wave, auto workgroup, auto* out) {
+    const int lane = (int)(16 / e) * kBwdUnroll;           // elements of a lane
+    const bool one = prob->V <= 64 * lane;
+    const int64_t parts = one ? 1 : (prob->V + 256 * lane - 1) / (256 * lane), wgs = one ? (n + 3) / 4 : n * parts;
+    if (wgs >= int64_t(1) << 32) return BGPO_ERR_UNSUPPORTED;
+    (one ? wave : workgroup)<<<line_grid(wgs), 256, 0, s>>>(p, (int)parts, lse, entropy, dlogp, dentropy, out, ldo);
     return hipGetLastError() == hipSuccess ? BGPO_OK : BGPO_ERR_HIP;
   };
   auto choose = [&](auto* out) {
     typedef std::remove_pointer_t<decltype(out)> T;
     const int64_t bytes = n * prob->V * e;
     if (bytes > kStreamLogits)
-      return dentropy ? launch(k_logits_logp_bwd<T, true, true, true>, out) : launch(k_logits_logp_bwd<T, false, true, true>, out);
+      return dentropy ? launch(k_logits_logp_bwd<T, true, true, true, 64>, k_logits_logp_bwd<T, true, true, true, 256>, out)
+                      : launch(k_logits_logp_bwd<T, false, true, true, 64>, k_logits_logp_bwd<T, false, true, true, 256>, out);
     if (bytes > kStreamGradient)
-      return dentropy ? launch(k_logits_logp_bwd<T, true, false, true>, out) : launch(k_logits_logp_bwd<T, false, false, true>, out);
-    return dentropy ? launch(k_logits_logp_bwd<T, true, false, false>, out) : launch(k_logits_logp_bwd<T, false, false, false>, out);
+      return dentropy ? launch(k_logits_logp_bwd<T, true, false, true, 64>, k_logits_logp_bwd<T, true, false, true, 256>, out)
+                      : launch(k_logits_logp_bwd<T, false, false, true, 64>, k_logits_logp_bwd<T, false, false, true, 256>, out);
+    return dentropy ? launch(k_logits_logp_bwd<T, true, false, false, 64>, k_logits_logp_bwd<T, true, false, false, 256>, out)
+                    : launch(k_logits_logp_bwd<T, false, false, false, 64>, k_logits_logp_bwd<T, false, false, false, 256>, out);
   };
   return f32 ? choose(static_cast<float*>(dlogits)) : choose(static_cast<uint16_t*>(dlogits));
 }

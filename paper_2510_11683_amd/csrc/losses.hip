@@ -79,7 +79,9 @@ __device__ __forceinline__ ExpParts exp_parts(double x) {
   s = fma_const(s, f, 1.0 / 24.0);
   s = fma_const(s, f, 1.0 / 6.0);
   s = fma(s, f, 0.5);
-  return ExpParts{fma(s * f, f, f), (int)n};
+  int k;
+  asm("v_cvt_i32_f64 %0, %1" : "=v"(k) : "v"(n));   // (saturates, NaN to 0: a cast has no value there)
+  return ExpParts{fma(s * f, f, f), k};
 }
 __device__ __forceinline__ double exp64(double x) {
   const ExpParts e = exp_parts(x);
@@ -199,11 +201,6 @@ struct Positions {
         if (live[u]) v[u] = p[i + u * G];
       }
     }
-  }
-  template <typename T>
-  __device__ __forceinline__ void select(T (&v)[U]) const {
-#pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = live[u] ? v[u] : (T)0;
   }
   template <typename T>
   __device__ __forceinline__ void store(T* p, int i, int end, const T (&v)[U]) const {
