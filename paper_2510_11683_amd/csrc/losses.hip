@@ -225,9 +225,10 @@ struct Range {
   int n, first, last;       // positions that count; all of them lie in [first, last)
 };
 
-// of [i0, end), in every lane of the workgroup of G
+// of [i0, end), in every one of G lanes (whole waves; all of the workgroup's call it,
+// each G with its own `red` of a row per wave)
 template <int G>
-__device__ __forceinline__ Range find_range(const uint8_t* mask, int i0, int end, int (*red)[3]) {
+__device__ __forceinline__ Range find_range(const uint8_t* mask, int i0, int end, int lane, int (*red)[3]) {
   if (!mask) return Range{end - i0, i0, end};
   int n = 0, first = end, last = i0;
   auto word = [&](uint32_t w, int at) {
@@ -238,7 +239,7 @@ __device__ __forceinline__ Range find_range(const uint8_t* mask, int i0, int end
     last = max(last, at + 4 - (__clz((int)t) >> 3));
   };
 #pragma unroll 2
-  for (int j = i0 + (int)threadIdx.x * 16; j < end; j += G * 16) {
+  for (int j = i0 + lane * 16; j < end; j += G * 16) {
     if (j + 16 <= end) {
       const raw16b w = *reinterpret_cast<const raw16b*>(mask + j);
 #pragma unroll
@@ -253,11 +254,10 @@ __device__ __forceinline__ Range find_range(const uint8_t* mask, int i0, int end
     first = min(first, __shfl_xor(first, off, 64));
     last = max(last, __shfl_xor(last, off, 64));
   }
-  const int wave = threadIdx.x >> 6;
-  if ((threadIdx.x & 63) == 0) {
-    red[wave][0] = n;
-    red[wave][1] = first;
-    red[wave][2] = last;
+  if ((lane & 63) == 0) {
+    red[lane >> 6][0] = n;
+    red[lane >> 6][1] = first;
+    red[lane >> 6][2] = last;
   }
   __syncthreads();
   n = 0;
@@ -300,11 +300,11 @@ struct Quad {
 };
 __device__ __forceinline__ bool live(uint32_t m, int e) { return (m >> (8 * e) & 255) != 0; }
 
-// p[a .. b) = 0, by the workgroup of G
+// p[a .. b) = 0, by G lanes
 template <int G, typename T>
-__device__ __forceinline__ void fill_zero(T* p, int a, int b) {
+__device__ __forceinline__ void fill_zero(T* p, int a, int b, int lane) {
   const T z[4] = {0, 0, 0, 0};
-  for (int i = a + (int)threadIdx.x * 4; i < b; i += G * 4) {
+  for (int i = a + lane * 4; i < b; i += G * 4) {
     if (i + 4 <= b) store4(p + i, z);
     else
       for (int k = i; k < b; ++k) p[k] = 0;
@@ -594,7 +594,7 @@ __device__ __forceinline__ double long_rows_pass(const PolicyArgs& p, int (*ired
   double count = 0.0;
   for (uint32_t k = blockIdx.x; k < p.pieces(); k += gridDim.x) {
     const int b = (int)(k / (uint32_t)p.n_chunks), i0 = (int)(k % (uint32_t)p.n_chunks) * p.chunk;
-    const Range r = find_range<G>(p.mask + b * p.ld_mask, i0, min(p.L, i0 + p.chunk), ired);
+    const Range r = find_range<G>(p.mask + b * p.ld_mask, i0, min(p.L, i0 + p.chunk), threadIdx.x, ired);
     double v[1] = {0.0};
     if (!TOKEN && p.old && r.n) {
       v[0] = range_log_ratio<T, G>(p, b, r);
@@ -624,7 +624,7 @@ __device__ __forceinline__ void long_loss_pass(const PolicyArgs& p, double w, do
     const T* ref = static_cast<const T*>(p.ref) + b * p.ld_ref;
     const float* adv = p.adv + b * p.ld_adv;
     T* dlogp = static_cast<T*>(p.dlogp) + b * p.ld_dlogp;
-    const Range r = find_range<G>(mask, i0, end, ired);
+    const Range r = find_range<G>(mask, i0, end, threadIdx.x, ired);
     double v[2] = {(double)r.n, 0.0};     // positions and sum of d of the response
     if (p.whole_rows()) {
       if (p.rows) {
@@ -645,8 +645,8 @@ __device__ __forceinline__ void long_loss_pass(const PolicyArgs& p, double w, do
     PolicySums s;
     if (!TOKEN && threadIdx.x == 0 && i0 == 0) s.d = v[1];
     if (p.dlogp) {
-      fill_zero<G>(dlogp, i0, r.first);
-      fill_zero<G>(dlogp, r.last, end);
+      fill_zero<G>(dlogp, i0, r.first, threadIdx.x);
+      fill_zero<G>(dlogp, r.last, end, threadIdx.x);
     }
     // a step's loads are issued before the step before it is computed and stored
     auto load = [&](Tile& t, int i) {
@@ -981,27 +981,30 @@ __device__ __forceinline__ void pair_terms(const PrefArgs& p, int q, int i0, int
   }
 }
 
-// The sum over a long row's range.
-template <typename T, int G, bool MASK, bool REF>
-__device__ __forceinline__ double range_score(const PrefArgs& p, const PrefSide& s, int q, const Range& r) {
+// Long rows: a pair to a workgroup, each response to one half of it.
+constexpr int kPairThreads = 2 * kThreads;
+
+// The sum over a response's range, per lane of its half.
+template <typename T, bool MASK, bool REF>
+__device__ __forceinline__ double range_score(const PrefArgs& p, const PrefSide& s, int q, int lane, const Range& r) {
   const uint8_t* mask = s.mask + q * s.ld_mask;
   const T* theta = static_cast<const T*>(s.theta) + q * s.ld;
   const T* ref = static_cast<const T*>(s.ref) + q * s.ld_ref;
   double sum = 0.0;
   constexpr int U = 4;
-  for (int j = r.first + (int)threadIdx.x * 4; j < r.last; j += G * 4 * U) {
+  for (int j = r.first + lane * 4; j < r.last; j += kThreads * 4 * U) {
     T x[U][4], o[U][4];
     uint32_t m[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const Quad k(j + u * G * 4, p.L);
+      const Quad k(j + u * kThreads * 4, p.L);
       m[u] = MASK ? k.mask(mask) : 0x01010101u;
       load4(theta + k.at, x[u]);
       if (REF) load4(ref + k.at, o[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      m[u] = Quad(j + u * G * 4, p.L).keep(m[u], r.last);
+      m[u] = Quad(j + u * kThreads * 4, p.L).keep(m[u], r.last);
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum += !live(m[u], e) ? 0.0 : REF ? (double)x[u][e] - (double)o[u][e] : (double)x[u][e];
     }
@@ -1009,40 +1012,34 @@ __device__ __forceinline__ double range_score(const PrefArgs& p, const PrefSide&
   return sum;
 }
 
-// Sum and unmasked positions of a long row's piece of both responses, in every
-// lane of the workgroup, and their ranges.
-template <typename T, int G>
-__device__ __forceinline__ void long_pair_terms(const PrefArgs& p, int q, int i0, int end, Range (&range)[2], double (&v)[4],
-                                                double (*red)[2], int (*ired)[3]) {
-  double d[2];
-#pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const PrefSide& s = p.side[c];
-    range[c] = find_range<G>(s.mask ? s.mask + q * s.ld_mask : nullptr, i0, end, ired);
-  }
-#pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const PrefSide& s = p.side[c];
-    d[c] = s.mask ? s.ref ? range_score<T, G, true, true>(p, s, q, range[c]) : range_score<T, G, true, false>(p, s, q, range[c])
-                  : s.ref ? range_score<T, G, false, true>(p, s, q, range[c]) : range_score<T, G, false, false>(p, s, q, range[c]);
-  }
-  group_sum<G, 2>(d, red);
-#pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    v[2 * c] = d[c];
-    v[2 * c + 1] = (double)range[c].n;
-  }
+// Sum and unmasked positions of a piece of both responses, in every lane, and the
+// range of the lane's own.
+template <typename T>
+__device__ __forceinline__ Range long_pair_terms(const PrefArgs& p, const PrefSide& s, int c, int q, int i0, int end,
+                                                 double (&v)[4], double (*red)[4], int (*ired)[3]) {
+  const int lane = threadIdx.x % kThreads;
+  const Range r = find_range<kThreads>(s.mask ? s.mask + q * s.ld_mask : nullptr, i0, end, lane, ired + c * (kThreads / 64));
+  const double d = s.mask ? s.ref ? range_score<T, true, true>(p, s, q, lane, r) : range_score<T, true, false>(p, s, q, lane, r)
+                          : s.ref ? range_score<T, false, true>(p, s, q, lane, r) : range_score<T, false, false>(p, s, q, lane, r);
+  const double n = lane == 0 ? (double)r.n : 0.0;
+  v[0] = c ? 0.0 : d;
+  v[1] = c ? 0.0 : n;
+  v[2] = c ? d : 0.0;
+  v[3] = c ? n : 0.0;
+  group_sum<kPairThreads, 4>(v, red);
+  return r;
 }
 
-// g at the positions of a long row's range that count, 0 at the others of the
+// g at the positions of a response's range that count, 0 at the others of the
 // piece.
-template <typename T, int G>
+template <typename T>
 __device__ __forceinline__ void range_gradient(const PrefArgs& p, const PrefSide& s, int q, int i0, int end, const Range& r, T g) {
+  const int lane = threadIdx.x % kThreads;
   T* grad = static_cast<T*>(s.grad) + q * s.ld_grad;
-  fill_zero<G>(grad, i0, r.first);
-  fill_zero<G>(grad, r.last, end);
+  fill_zero<kThreads>(grad, i0, r.first, lane);
+  fill_zero<kThreads>(grad, r.last, end, lane);
   const uint8_t* mask = s.mask + q * s.ld_mask;
-  for (int j = r.first + (int)threadIdx.x * 4; j < r.last; j += G * 4) {
+  for (int j = r.first + lane * 4; j < r.last; j += kThreads * 4) {
     const Quad k(j, p.L);
     const uint32_t m = r.n == r.last - r.first ? 0x01010101u : k.mask(mask);
     T o[4];
@@ -1054,14 +1051,14 @@ __device__ __forceinline__ void range_gradient(const PrefArgs& p, const PrefSide
 
 // First pass: these terms of every piece.
 template <typename T, int G>
-__device__ __forceinline__ void scores_pass(const PrefArgs& p, int group, int n_groups, double (*red)[2], int (*ired)[3]) {
+__device__ __forceinline__ void scores_pass(const PrefArgs& p, int group, int n_groups, double (*red)[4], int (*ired)[3]) {
   for (uint32_t k = group; k < p.pieces(); k += n_groups) {
     const int q = (int)(k / (uint32_t)p.n_chunks), i0 = (int)(k % (uint32_t)p.n_chunks) * p.chunk;
     const int end = min(p.L, i0 + p.chunk);
     double v[4];
     if constexpr (G > 64) {
-      Range r[2];
-      long_pair_terms<T, G>(p, q, i0, end, r, v, red, ired);
+      const int c = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads);
+      long_pair_terms<T>(p, p.side[c], c, q, i0, end, v, red, ired);
     } else {
       pair_terms<T, G>(p, q, i0, end, v);
       group_sum<G, 4>(v, nullptr);
@@ -1082,18 +1079,19 @@ __device__ __forceinline__ void pairs_pass(const PrefArgs& p, int group, int n_g
     const int q = (int)(k / (uint32_t)p.n_chunks), i0 = (int)(k % (uint32_t)p.n_chunks) * p.chunk;
     const int end = min(p.L, i0 + p.chunk);
     double v[4] = {0.0, 0.0, 0.0, 0.0};
-    Range range[2];
+    Range range;
+    const int half = G > 64 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads) : 0;
+    const PrefSide& own = p.side[half];
     if (p.scores) {
       if constexpr (G > 64)
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-          range[c] = find_range<G>(p.side[c].mask ? p.side[c].mask + q * p.side[c].ld_mask : nullptr, i0, end, ired);
+        range = find_range<kThreads>(own.mask ? own.mask + q * own.ld_mask : nullptr, i0, end, threadIdx.x % kThreads,
+                                     ired + half * (kThreads / 64));
       for (int c = lane; c < p.n_chunks; c += G)
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] += p.scores[((int64_t)q * p.n_chunks + c) * 4 + e];
       group_sum<G, 4>(v, red);
     } else if constexpr (G > 64) {
-      long_pair_terms<T, G>(p, q, i0, end, range, v, reinterpret_cast<double(*)[2]>(red), ired);
+      range = long_pair_terms<T>(p, own, half, q, i0, end, v, red, ired);
     } else {
       pair_terms<T, G>(p, q, i0, end, v);
       group_sum<G, 4>(v, red);
@@ -1116,12 +1114,12 @@ __device__ __forceinline__ void pairs_pass(const PrefArgs& p, int group, int n_g
       bad = bad || !isfinite((float)g) || !isfinite(g_side[0]) || !isfinite(g_side[1]);
     }
     if (!p.side[0].grad) continue;
+    if constexpr (G > 64) {
+      range_gradient<T>(p, own, q, i0, end, range, half ? g_side[1] : g_side[0]);
+    } else {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const PrefSide& s = p.side[c];
-      if constexpr (G > 64) {
-        range_gradient<T, G>(p, s, q, i0, end, range[c], g_side[c]);
-      } else {
+      for (int c = 0; c < 2; ++c) {
+        const PrefSide& s = p.side[c];
         const uint8_t* mask = s.mask ? s.mask + q * s.ld_mask : nullptr;
         T* grad = static_cast<T*>(s.grad) + q * s.ld_grad;
         for (int j = i0; j < end; j += G * 4) {
@@ -1143,17 +1141,19 @@ __device__ void write_pref_stats(const PrefArgs& p, const double (&s)[kPrefSums]
   if (!isfinite(s[0]) && p.flags) atomicOr(p.flags, kFlagNonfinite);
 }
 
+constexpr int pair_threads(int G) { return G > 64 ? G : kThreads; }
+
 template <typename T, int G>
-__global__ __launch_bounds__(kThreads) void k_preference_scores(PrefArgs p) {
-  constexpr int kWg = kThreads, kGroups = kWg / G;
-  __shared__ double red[kWg / 64][2];
+__global__ __launch_bounds__(pair_threads(G)) void k_preference_scores(PrefArgs p) {
+  constexpr int kWg = pair_threads(G), kGroups = kWg / G;
+  __shared__ double red[kWg / 64][4];
   __shared__ int ired[kWg / 64][3];
   scores_pass<T, G>(p, blockIdx.x * kGroups + group_index<G, kWg>(), gridDim.x * kGroups, red, ired);
 }
 
 template <typename T, int G>
-__global__ __launch_bounds__(kThreads) void k_preference(PrefArgs p) {
-  constexpr int kWg = kThreads, kGroups = kWg / G;
+__global__ __launch_bounds__(pair_threads(G)) void k_preference(PrefArgs p) {
+  constexpr int kWg = pair_threads(G), kGroups = kWg / G;
   __shared__ double red[kWg / 64][4];
   double sums[kPrefSums] = {0.0, 0.0, 0.0};
   bool bad = false;
@@ -1219,7 +1219,7 @@ static size_t preference_bytes(const PolicyPlan& q) {
 
 template <typename T, int G>
 static int launch_preference(const PrefArgs& p, const PolicyPlan& q, hipStream_t s) {
-  constexpr int kWg = kThreads, kGroups = kWg / G;
+  constexpr int kWg = pair_threads(G), kGroups = kWg / G;
   const unsigned wgs = (unsigned)std::min<int64_t>((q.pieces + kGroups - 1) / kGroups, kMaxWgs);
   if (p.scores) {
     k_preference_scores<T, G><<<wgs, kWg, 0, s>>>(p);
@@ -1241,7 +1241,7 @@ static int run_preference(const PrefArgs& p, const PolicyPlan& q, hipStream_t s)
   switch (q.lanes) {
     case 16: return launch_preference<T, 16>(p, q, s);
     case 64: return launch_preference<T, 64>(p, q, s);
-    default: return launch_preference<T, kThreads>(p, q, s);
+    default: return launch_preference<T, kPairThreads>(p, q, s);
   }
 }
 
