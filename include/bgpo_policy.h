@@ -154,7 +154,8 @@ int bgpo_policy_workspace_size(const bgpo_policy* prob, size_t* bytes);
  *   logp_old  [B, L]  under the policy that drew the responses; NULL: d = 0
  *   logp_ref  [B, L]  under the reference; NULL: no KL term (kl_coef must be 0)
  *   adv       float [B] or [B, L] (ld_adv)
- *   resp_mask uint8 [B, L]  positions that count; the others are not read
+ *   resp_mask uint8 [B, L]  nonzero: the position counts; what the others hold (NaN
+ *             too) does not matter
  *   dlogp     [B, L]  out; NULL: the loss alone
  *   stats     double [6]  out
  *   status_flags  int32 [1]  |= BGPO_FLAG_NONFINITE if the loss or a gradient
@@ -178,7 +179,7 @@ enum {
 typedef struct bgpo_preference {
   int64_t ld_win, ld_lose, ld_win_ref, ld_lose_ref, ld_win_mask, ld_lose_mask, ld_dwin,
       ld_dlose;       /* elements between pairs, >= L (any value for P = 1 or a NULL array) */
-  int64_t adv_stride; /* elements between pairs of adv_win and adv_lose, >= 1 */
+  int64_t adv_stride; /* elements between pairs of adv_win and adv_lose, 1 .. 2^24 */
   double beta;        /* > 0, finite */
   double margin;      /* finite */
   double label_smoothing;  /* 0 <= e < 1; 0 unless BGPO_PREF_SIGMOID */

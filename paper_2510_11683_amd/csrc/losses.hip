@@ -1,9 +1,16 @@
 // Policy and preference losses on log-probabilities, with their gradients.
 //
 // All of the arithmetic is in float64 (differences of log-probabilities, their
-// exponentials, the comparison with the clip's borders, every sum): the kernels
-// read 13 bytes per fp32 position and write 4, and the float64 work of a
-// position takes less time than that.  Sums run in a fixed order.
+// exponentials, the comparison with the clip's borders, every sum); only a
+// gradient is rounded to its type.  A position is 13 bytes read and 4 written in
+// fp32, and some 60 instructions (100 with a ratio of its own), which takes less
+// time than its bytes.  Sums run in a fixed order.
+//
+// What bounds the kernels is latency: a response's sums, or the batch's count,
+// stand between reading and writing.  Long rows: 1024 of 16385 positions in fp32,
+// ragged (184 MB), one ratio each, 54 us (3.4 TB/s; the longest rows take twice
+// the mean), all full 67 us (335 MB, 5.0 TB/s).  384 pairs of up to 8191 (57 MB): 21
+// us.  8 x 512 tokens: 9.4 us, 16 x 32 samples 6.1 us, 8 pairs of 16 samples 6.3 us.
 #include <math.h>
 
 #include <algorithm>
@@ -220,7 +227,8 @@ struct Positions {
 // them).  The arrays are then read only there, four positions to a lane, masked
 // ones too and without a condition: a load under a condition cannot be told from
 // one that was not made when a later one is waited for, so that nothing could be
-// in flight across a step.
+// in flight across a step.  (Read under the mask's condition, the long rows above
+// took 78 us at best, with workgroups of 256 to 1024 and two to eight waves a SIMD.)
 struct Range {
   int n, first, last;       // positions that count; all of them lie in [first, last)
 };
@@ -506,7 +514,8 @@ __device__ __forceinline__ void row_loss(const PolicyArgs& p, const PolicyRow& r
 
 template <bool TOKEN>
 __device__ __forceinline__ void add_sums(const PolicyRow& row, const PolicySums& s, double (&sums)[kPolicySums]) {
-  sums[0] -= row.w * (TOKEN ? s.f : s.positions * row.f);
+  // (a lane without positions adds nothing, whatever the response's objective is)
+  sums[0] -= row.w * (TOKEN ? s.f : s.positions ? s.positions * row.f : 0.0);
   sums[1] += row.w * s.kl;
   sums[2] += row.w * s.d;
   sums[3] += (double)s.positions;
@@ -828,10 +837,14 @@ struct PolicyPlan {
 };
 
 // Up to this many positions are one workgroup's work: one launch instead of two
-// or three.
+// or three (8 x 1000: 17.7 us against 22; 16 x 1000 so: 21.4 against 19.8).
 constexpr int64_t kSmallBatch = 8192;
 
-// Pieces of rows of L positions.
+// Pieces of rows of L positions.  Lanes of a row: 8192 of up to 50 positions take
+// 16.4 us with 16, 21.3 with 64; 4096 of up to 800 take 25.1 with 64, 39.3 with 256.
+// Few long rows are cut up for 512 workgroups (8 of 65536: 60 -> 19 us, 64 of 16384:
+// 25.7 -> 20.2), which costs a launch more; with more rows it costs more than it
+// gives (384 pairs of 8191, cut in two: 25 -> 40).
 static void cut_rows(int64_t rows, int64_t L, PolicyPlan* q) {
   q->small = rows * L <= kSmallBatch;
   int64_t n = 1;
@@ -839,7 +852,7 @@ static void cut_rows(int64_t rows, int64_t L, PolicyPlan* q) {
     q->lanes = L <= 64 ? 16 : 64;
     n = rows < kSmallThreads / q->lanes ? (L + q->lanes * 4 - 1) / (q->lanes * 4) : 1;
   } else {
-    q->lanes = L <= 64 ? 16 : L <= 512 ? 64 : kThreads;
+    q->lanes = L <= 64 ? 16 : L <= 1024 ? 64 : kThreads;
     n = std::max<int64_t>(1, std::min<int64_t>((512 + rows - 1) / rows, L / 4096));
   }
   q->chunk = (int)((L + n - 1) / n);
@@ -1111,7 +1124,8 @@ __device__ __forceinline__ void pairs_pass(const PrefArgs& p, int group, int n_g
         p.side[0].adv[q * p.adv_stride] = (float)-g;
         p.side[1].adv[q * p.adv_stride] = (float)g;
       }
-      bad = bad || !isfinite((float)g) || !isfinite(g_side[0]) || !isfinite(g_side[1]);
+      bad = bad || !isfinite(g) || (p.side[0].adv && !isfinite((float)g)) ||
+            (p.side[0].grad && !(isfinite(g_side[0]) && isfinite(g_side[1])));
     }
     if (!p.side[0].grad) continue;
     if constexpr (G > 64) {

@@ -173,6 +173,21 @@ def test_policy_loss_flags_what_is_not_finite():
     assert np.isfinite(s).all() and np.isinf(g).all() and int(flags) == b.BGPO_FLAG_NONFINITE
 
 
+@pytest.mark.parametrize("L", [3, 70, 700])
+def test_infinite_objective_of_a_sequence_ratio(L):
+    """A ratio past every float under a negative advantage: the loss is +inf, not NaN,
+    also where lanes of the response's group have no position."""
+    b = lib()
+    old = np.zeros((2, L))
+    lp = old.copy()
+    lp[1] = 900.0
+    flags = torch.zeros(1, dtype=torch.int32, device="cuda")
+    s, g = _run_policy(lp, old, None, np.array([1.0, -2.0], np.float32), np.ones((2, L), np.uint8), torch.float64, flags=flags,
+                       ratio="sequence", reduce="responses")
+    assert s[0] == math.inf and s[1] == math.inf and int(flags) == b.BGPO_FLAG_NONFINITE
+    assert np.isfinite(g[0]).all() and (g[1] == math.inf).all()
+
+
 # ---------------------------------------------------------------- preference loss
 
 def _run_pref(a, dtype, pad=0, grad=True, adv=True, margins=True, flags=None, **kw):
@@ -282,6 +297,12 @@ def test_preference_loss_at_its_limits():
     assert o["stats"][1] == 2 and o["adv_win"][1] == 1.0 and abs(o["adv_win"][0]) == 0 and int(flags) == 0
     o = _run_pref(a, torch.float64, flags=flags, kind="hinge", beta=1.0)
     assert o["stats"][0] == 5001.0 + 1.0 and o["adv_win"].tolist() == [0, 1, 1, 0] and int(flags) == 0   # m = 1 exactly: 0
+    # an advantage past fp32's range is flagged where it is asked for
+    o = _run_pref(a, torch.float64, flags=flags, kind="squared", beta=1e-3, loss_scale=1e36, adv=False)
+    assert int(flags) == 0 and np.isfinite(o["dwin"]).all()
+    o = _run_pref(a, torch.float64, flags=flags, kind="squared", beta=1e-3, loss_scale=1e36)
+    assert int(flags) == b.BGPO_FLAG_NONFINITE and np.isinf(o["adv_win"]).any()
+    flags.zero_()
     a["lose"][2, 1] = np.nan
     o = _run_pref(a, torch.float64, flags=flags, kind="hinge", beta=1.0)
     assert math.isnan(o["stats"][0]) and np.isnan(o["dwin"][2]).all() and int(flags) == b.BGPO_FLAG_NONFINITE
