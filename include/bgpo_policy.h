@@ -48,7 +48,7 @@ typedef struct bgpo_logits {
   int64_t ld;         /* elements between rows, >= V (any value for one row) */
   int32_t V;          /* 1 <= V <= 2^24 */
   int32_t in_dtype;   /* BGPO_BF16 or BGPO_F32 */
-  float scale;        /* > 0, finite */
+  float scale;        /* > 0, <= 2^64 */
   int32_t reserved;   /* 0 */
 } bgpo_logits;
 
@@ -73,7 +73,10 @@ int bgpo_logits_logp(const bgpo_logits* prob, const void* logits, const int32_t*
 /* Gradient of a scalar w.r.t. the logits, from its gradients w.r.t. logp (a)
  * and the entropy (b):
  *   dlogits_v = scale (a (1[v = y] - p_v) - b p_v (log p_v + H))
- *   lse       float [rows]   of bgpo_logits_logp with the same scale
+ *   lse       float [rows]   of bgpo_logits_logp with the same scale: p =
+ *             e^(z - lse), off by the rounding of lse, 2^-24 |lse| of p.  A row
+ *             with |lse| of 1024 or more (a row of nothing but the type's lowest
+ *             value, say) is summed again from its logits
  *   entropy   float [rows]   of the same call; may be NULL without dentropy
  *   dlogp     float [rows]   a
  *   dentropy  float [rows]   b; NULL = 0

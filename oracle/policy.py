@@ -30,7 +30,8 @@ def logits_logp(x, targets, row_mask=None, scale=1.0):
 
 
 def logits_logp_bwd(x, targets, lse, entropy, dlogp, dentropy=None, row_mask=None, scale=1.0):
-    """d (sum_r dlogp_r logp_r + dentropy_r H_r) / d x, with the given statistics."""
+    """d (sum_r dlogp_r logp_r + dentropy_r H_r) / d x, with the given statistics
+    (lse where it is below 1024; a rounded one has not the digits of p beyond)."""
     x = np.asarray(x, dtype=np.float64)
     g = np.zeros_like(x)
     for r, y in enumerate(targets):
@@ -41,6 +42,9 @@ def logits_logp_bwd(x, targets, lse, entropy, dlogp, dentropy=None, row_mask=Non
             g[r] = np.nan
             continue
         lp = x[r] * scale - float(lse[r])
+        if abs(lse[r]) >= 1024:
+            z = x[r] * scale
+            lp = z - z.max() - np.log(np.exp(z - z.max()).sum())
         p = np.exp(lp)
         g[r] = -a * p
         g[r, y] += a

@@ -498,8 +498,8 @@ def _workspace_args(ws: Optional[torch.Tensor], device: int):
 
 def _logits_problem(logits, scale: float, device: int):
     """(the bgpo_logits, address, rows, V)"""
-    if logits.dim() != 2:
-        raise ValueError("logits must be a matrix [rows, V]")
+    if logits is None or logits.dim() != 2 or logits.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("logits must be a matrix [rows, V] in bf16 or fp32")
     rows, V = logits.shape
     at, ld = (None, V) if rows == 0 else _mat(logits, "logits", (torch.bfloat16, torch.float32), rows, V, device)
     return _LOGITS.pack(rows, ld, V, BGPO_F32 if logits.dtype == torch.float32 else BGPO_BF16, scale, 0), at, rows, V
@@ -673,7 +673,8 @@ def bgpo_preference_loss(prob: PreferenceLoss, win, lose, win_ref, lose_ref, win
 class GradList:
     """A list of gradients in the form that bgpo_grad_norm and bgpo_grad_clip
     take; keeps the tensors.  Built once and used again: every call looks up
-    where the tensors are, and takes in anew what has moved."""
+    where the tensors are, and takes in anew what has moved (a tensor that is
+    resized or retyped where it stands needs a new list)."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)

@@ -136,6 +136,37 @@ __device__ __forceinline__ RowStats join_wave(RowStats a, float c) {
   return a;
 }
 
+// Statistics of x[i0, end), per lane: kUnroll 16-byte loads to a step, whose
+// logits share one maximum.
+constexpr int kUnroll = 4;
+
+template <typename T, bool ENT, bool NT, int LANES>
+__device__ __forceinline__ RowStats scan(const T* x, int i0, int end, int lane, float c) {
+  constexpr int N = Elem<T>::N;
+  RowStats a{-INFINITY, 0.f, 0.f};
+  int i = i0 + lane * N;
+  for (; i + (kUnroll - 1) * LANES * N + N <= end; i += kUnroll * LANES * N) {
+    raw16 raw[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) raw[u] = load16<NT>(x + i + u * LANES * N);
+    float f[kUnroll][N];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) Elem<T>::unpack(raw[u], f[u]);
+    add<ENT>(a, reinterpret_cast<float(&)[kUnroll * N]>(f), c);
+  }
+  for (; i + N <= end; i += LANES * N) {
+    float f[N];
+    Elem<T>::unpack(load16<NT>(x + i), f);
+    add<ENT>(a, f, c);
+  }
+  i = i0 + (end - i0) / N * N + lane;
+  if (i < end) {
+    const float f[1] = {Elem<T>::one(x[i])};
+    add<ENT>(a, f, c);
+  }
+  return a;
+}
+
 struct LogitRows {
   const void* x;
   const int32_t* targets;
@@ -159,13 +190,10 @@ __device__ void finish_row(const LogitRows& p, int64_t r, int y, const RowStats&
 }
 
 // A row, or one of the n_parts pieces of `chunk` logits that a row is cut into,
-// to a workgroup (LANES 256) or a wave (64): kUnroll 16-byte loads to a lane and
-// step, whose logits share one maximum.  Pieces go to `part` and are joined by
+// to a workgroup (LANES 256) or a wave (64).  Pieces go to `part` and are joined by
 // k_logits_join.  Bound by HBM: 4096 rows of 126464 in bf16, a fifth masked, with
 // entropies 138 us (6.0 TB/s), of which its vector work (8 instructions to a logit,
 // 32 cycles of a wave) would take 60 %.
-constexpr int kUnroll = 4;
-
 template <typename T, bool ENT, bool NT, int LANES>
 __global__ __launch_bounds__(256) void k_logits_logp(LogitRows p, int n_parts, int chunk, RowStats* __restrict__ part,
                                                      float* __restrict__ logp, float* __restrict__ entropy,
@@ -187,27 +215,7 @@ __global__ __launch_bounds__(256) void k_logits_logp(LogitRows p, int n_parts, i
   const int i0 = (int)(item % (unsigned)n_parts) * chunk, end = min(p.V, i0 + chunk);
   const T* x = static_cast<const T*>(p.x) + r * p.ld;
   const float c = p.scale * kLog2e;
-  RowStats a{-INFINITY, 0.f, 0.f};
-  int i = i0 + lane * N;
-  for (; i + (kUnroll - 1) * LANES * N + N <= end; i += kUnroll * LANES * N) {
-    raw16 raw[kUnroll];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) raw[u] = load16<NT>(x + i + u * LANES * N);
-    float f[kUnroll][N];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) Elem<T>::unpack(raw[u], f[u]);
-    add<ENT>(a, reinterpret_cast<float(&)[kUnroll * N]>(f), c);
-  }
-  for (; i + N <= end; i += LANES * N) {
-    float f[N];
-    Elem<T>::unpack(load16<NT>(x + i), f);
-    add<ENT>(a, f, c);
-  }
-  i = i0 + (end - i0) / N * N + lane;
-  if (i < end) {
-    const float f[1] = {Elem<T>::one(x[i])};
-    add<ENT>(a, f, c);
-  }
+  RowStats a = scan<T, ENT, NT, LANES>(x, i0, end, lane, c);
   a = join_wave<ENT>(a, c);
   if constexpr (LANES == 256) {
     if ((lane & 63) == 0) red[lane >> 6] = a;
@@ -250,6 +258,44 @@ __global__ __launch_bounds__(256) void k_logits_join(LogitRows p, int n_parts, c
 // four 310, eight 552).
 constexpr int kBwdUnroll = 2;
 
+// From this magnitude on lse has no longer the digits that p = e^(z - lse) needs
+// (its rounding is 2^-15 of p just below; ln S is lost in it altogether in a row of
+// nothing but the type's lowest value).
+constexpr float kFarLse = 1024.f;
+
+// The gradient of a whole row with such an lse, by LANES lanes: its maximum and
+// its sum are taken again from the logits, all of which are read before the first
+// is written.
+template <typename T, bool ENT, int LANES>
+__device__ __forceinline__ void far_row(const LogitRows& p, const T* x, T* o, int y, int lane, float a, float b, float h,
+                                        RowStats* red) {
+  constexpr int N = Elem<T>::N;
+  const float c = p.scale * kLog2e;
+  RowStats s = join_wave<false>(scan<T, false, false, LANES>(x, 0, p.V, lane, c), c);
+  if constexpr (LANES == 256) {
+    if ((lane & 63) == 0) red[lane >> 6] = s;
+    __syncthreads();
+    s = red[0];
+    for (int w = 1; w < 4; ++w) join<false>(s, red[w], c);
+  }
+  const float m = reference(s.m), ls = s.s > 0.f ? logf(s.s) : NAN;
+  auto grad = [&](float v, int i) -> float {
+    const float t = fmaf(v - m, p.scale, -ls), q = __builtin_amdgcn_exp2f(t * kLog2e);
+    float g = -q * a;
+    if (ENT) g = fmaf(-q * b, fmaxf(t, kNoExponent) + h, g);
+    return i == y ? g + a : g;
+  };
+  for (int i = lane * N; i + N <= p.V; i += LANES * N) {
+    float f[N];
+    Elem<T>::unpack(load16<false>(x + i), f);
+#pragma unroll
+    for (int e = 0; e < N; ++e) f[e] = grad(f[e], i + e);
+    store16<false>(o + i, Elem<T>::pack(f));
+  }
+  const int i = p.V / N * N + lane;
+  if (i < p.V) o[i] = Elem<T>::round(grad(Elem<T>::one(x[i]), i));
+}
+
 template <typename T, bool ENT, bool NTL, bool NTS, int LANES>
 __global__ __launch_bounds__(256) void k_logits_logp_bwd(LogitRows p, int n_parts, const float* __restrict__ lse,
                                                          const float* __restrict__ entropy,
@@ -257,6 +303,7 @@ __global__ __launch_bounds__(256) void k_logits_logp_bwd(LogitRows p, int n_part
                                                          const float* __restrict__ dentropy,
                                                          T* dlogits, int64_t ld_out) {
   constexpr int N = Elem<T>::N, kChunk = LANES * N * kBwdUnroll;
+  __shared__ RowStats red[4];
   const unsigned item = LANES == 256 ? line_index() : line_index() * 4 + (threadIdx.x >> 6);
   const int64_t r = item / (unsigned)n_parts;
   if (r >= p.rows) return;
@@ -289,6 +336,12 @@ __global__ __launch_bounds__(256) void k_logits_logp_bwd(LogitRows p, int n_part
     const int i = first + u * LANES * N;
     if (!none && i + N <= p.V) raw[u] = load16<NTL>(x + i);
   }
+  // Asked once the loads are out (before them: 299 us where this takes 289); what
+  // they have brought is not used then, and the row is its first piece's work.
+  if (__builtin_expect(!none && fabsf(l) >= kFarLse, 0)) {       // (row-uniform)
+    if (i0 == 0) far_row<T, ENT, LANES>(p, x, o, y, threadIdx.x % LANES, a, b, h, red);
+    return;
+  }
 #pragma unroll
   for (int u = 0; u < kBwdUnroll; ++u) {
     const int i = first + u * LANES * N;
@@ -318,7 +371,7 @@ static int check_logits(const bgpo_logits* p) {
   if (!p || p->rows < 0 || p->V < 1 || p->reserved || !(p->scale > 0.f) || !isfinite(p->scale) ||
       (p->in_dtype != BGPO_BF16 && p->in_dtype != BGPO_F32))
     return BGPO_ERR_INVALID_ARG;
-  if (p->rows >= int64_t(1) << 31 || p->V > 1 << 24) return BGPO_ERR_UNSUPPORTED;
+  if (p->rows >= int64_t(1) << 31 || p->V > 1 << 24 || p->scale > 0x1p64f) return BGPO_ERR_UNSUPPORTED;
   if (bad_stride(p, p->ld, p->rows, p->V)) return BGPO_ERR_INVALID_ARG;
   return BGPO_OK;
 }

@@ -189,6 +189,58 @@ def test_backward(rows, V, dtype):
         _check_bwd(x, y, yn, stats, a, c, mask, scale, dtype, in_place, ld_pad)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [3, 700, 2500, 40001])
+def test_backward_of_rows_far_from_zero(V, dtype):
+    """Rows whose lse in fp32 holds little or nothing of ln S: the type's lowest or
+    highest values everywhere, large offsets, an lse past the range of fp32.  The
+    gradient of the logits themselves in float64, forward and backward on the device.
+    Off by: p, (3 |t| + 6) 2^-24 and the sum's V / 64 + 16 + 3 (ln V + 1) roundings;
+    the entropy, the forward's tolerance."""
+    b = lib()
+    fi = torch.finfo(dtype)
+    rng = np.random.default_rng(V)
+    for scale in (1.0, 1.5):
+        rows = 7
+        x, _, y, yn = _make(rows, V, dtype, pad=1, offset=1)
+        x[0] = fi.min
+        x[1] = fi.max
+        x[2] += 5000.0
+        x[3] -= 40000.0
+        x[4] = fi.min
+        x[4, V // 2] = -1e30                  # one token is far above the others
+        x[5] = -2000.0
+        x[5, 0] = -math.inf
+        yn[5] = V - 1
+        y = torch.from_numpy(yn).cuda()
+        xf = x.float().cpu().numpy().astype(np.float64)
+        logp, ent, lse = (torch.empty(rows, device="cuda") for _ in range(3))
+        b.bgpo_logits_logp(x, y, logp, ent, lse, b.logits_workspace(rows, V), scale=scale)
+        a, c = (rng.standard_normal(rows).astype(np.float32) for _ in range(2))
+        s32 = float(np.float32(scale))
+        z = (xf - xf.max(1, keepdims=True)) * s32
+        lp = z - np.log(np.exp(z).sum(1, keepdims=True))
+        p = np.exp(lp)
+        h = -(p * np.where(p > 0, lp, 0.0)).sum(1)
+        want = -p * (a[:, None] + np.where(p > 0, c[:, None] * (lp + h[:, None]), 0.0))
+        want[np.arange(rows), yn] += a
+        want *= s32
+        n = (V / 64 + 16 + 3 * (math.log(V) + 1) + 2) * E24
+        t = np.clip(np.abs(lp), 0.0, 104.0)
+        pe = p * ((3 * t + 6) * E24 + n)
+        tol = np.abs(a)[:, None] * pe + np.abs(c)[:, None] * (pe * (t + h[:, None]) + p * (4 * (t + h[:, None]) * E24 + 2 * n * (math.log(V) + 2)))
+        tol = s32 * (tol + 4 * E24 * np.abs(a)[:, None] + 2.0 ** -126 * 128 * (np.abs(a) + np.abs(c))[:, None])
+        tol += np.abs(want) * (4 * E24 + (2.0 ** -8 if dtype == torch.bfloat16 else 0.0))
+        # (a lse below 1024 is taken as it is: 2^-24 |lse| of p more)
+        near = np.where(np.abs(xf.max(1) * s32) < 1100, np.abs(xf.max(1) * s32) + 20, 0.0)
+        tol += s32 * (near * E24)[:, None] * p * (np.abs(a)[:, None] + np.abs(c)[:, None] * (t + h[:, None] + 1))
+        for in_place in (False, True):
+            out = x if in_place else torch.full_like(x, 9.0)
+            b.bgpo_logits_logp_bwd(x, y, lse, ent, torch.from_numpy(a).cuda(), torch.from_numpy(c).cuda(), out, scale=scale)
+            err = np.abs(out.float().cpu().numpy().astype(np.float64) - want)
+            assert (err <= tol).all(), (scale, in_place, (err / tol).max(1))
+
+
 def test_backward_against_differences():
     """The kernels' own gradient against central differences of the kernels' own
     forward (fp32 logits, a step of 2^-5: the truncation is h^2 / 6 of a third

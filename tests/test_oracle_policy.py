@@ -36,6 +36,15 @@ def test_logits_match_torch_and_its_gradient():
     assert not g[3].any() and not g[5].any() and not g[2, 5:9].any()
 
 
+def test_logits_gradient_of_a_row_of_lowest_values():
+    """Uniform, however little of it an fp32 lse still holds."""
+    x = np.full((1, 8), np.finfo(np.float32).min)
+    logp, ent, lse = oracle.logits_logp(x, [3])
+    assert np.isclose(logp[0], -np.log(8)) and np.isclose(ent[0], np.log(8))
+    g = oracle.logits_logp_bwd(x, [3], lse.astype(np.float32), ent, [2.0])
+    assert np.allclose(g[0], 2.0 * (np.eye(8)[3] - 1 / 8))
+
+
 @pytest.mark.parametrize("ratio", ["token", "sequence"])
 @pytest.mark.parametrize("reduce", ["tokens", "responses", "sum"])
 def test_policy_loss_against_differences(ratio, reduce):

@@ -59,7 +59,7 @@ def _logp_bwd(b, prob, over=()):
 
 BAD_LOGITS = [(dict(rows=-1), INVALID), (dict(V=0), INVALID), (dict(V=-5), INVALID), (dict(ld=99), INVALID),
               (dict(in_dtype=2), INVALID), (dict(in_dtype=-1), INVALID), (dict(scale=0.0), INVALID),
-              (dict(scale=-1.0), INVALID), (dict(scale=math.nan), INVALID), (dict(scale=math.inf), INVALID),
+              (dict(scale=-1.0), INVALID), (dict(scale=math.nan), INVALID), (dict(scale=math.inf), INVALID), (dict(scale=2.0 ** 65), UNSUPPORTED),
               (dict(reserved=1), INVALID), (dict(rows=1 << 31), UNSUPPORTED),
               (dict(V=(1 << 24) + 1, ld=1 << 25), UNSUPPORTED), (dict(ld=(1 << 54) + 1), INVALID)]
 
