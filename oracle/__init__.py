@@ -10,6 +10,8 @@ Modules:
   elbo    the per-sample ELBO, the lower-bound term, the loss and its
           gradients, in a literal per-sample form and a collapsed form for
           hidden states shared across samples
+  policy  token log-probabilities of logits, policy and preference losses,
+          gradient norm
 
 Parity status: every function here is pinned by the CPU tests
 (known-answer vectors, closed forms, brute force, library routines, finite

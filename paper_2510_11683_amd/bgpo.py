@@ -1,4 +1,4 @@
-"""ctypes binding of libbgpo (include/bgpo.h).
+"""ctypes binding of libbgpo (the headers in include/).
 
 Argument marshalling only: tensors are checked for device, dtype, shape and
 contiguity and passed as raw device pointers together with torch's current

@@ -2,8 +2,8 @@
 //
 // The list travels in the kernels' arguments, up to kEntries tensors to a launch
 // (12 bytes each: an address of 48 bits, the elements of the last chunk, the type,
-// and the number of the first chunk).  The tensors are cut into chunks of kChunk
-// elements, numbered through the launch; a workgroup finds its chunk's tensor by
+// and the number of the first chunk).  The tensors are cut into chunks of 32 KB,
+// numbered through the launch; a workgroup finds its chunk's tensor by
 // bisection.
 #include <math.h>
 
@@ -20,7 +20,10 @@
 
 namespace bgpo {
 
-constexpr int64_t kChunk = 16384;
+// elements of a chunk (16384 fp32 elements to a chunk: clipping 534M into bf16 851 us,
+// 8192 820, 300M in place 198 and 200; 8192 bf16 elements: 250M in place 107, 16384 103)
+constexpr int64_t kChunkBytes = 32768;
+__host__ __device__ constexpr int64_t chunk_elements(bool f32) { return kChunkBytes / (f32 ? 4 : 2); }
 constexpr int kNormWgs = 1024;             // workgroups of a norm pass, one partial each
 constexpr int kMaxClipWgs = 1 << 22;
 constexpr int kEntries = 312, kPairs = 184;  // of a launch: gradients; gradients and outputs (4 KB of arguments)
@@ -37,10 +40,10 @@ struct Packed {
   __host__ __device__ int tail() const { return (int)(v & 0x3FFF) + 1; }
   static Packed of(const bgpo_tensor& t) {
     return Packed{(uint64_t)(uintptr_t)t.data << 16 | (uint64_t)(t.dtype == BGPO_F32) << 15 |
-                  (uint64_t)((t.n - 1) % kChunk)};
+                  (uint64_t)((t.n - 1) % chunk_elements(t.dtype == BGPO_F32))};
   }
 };
-static_assert(kChunk <= 1 << 14, "a chunk's elements are held in 14 bits");
+static_assert(chunk_elements(false) <= 1 << 14, "a chunk's elements are held in 14 bits");
 
 template <int N, bool OUT>
 struct Table {
@@ -61,14 +64,16 @@ struct Table {
     return lo;
   }
   // where chunk c of entry e starts and how long it is
-  __device__ __forceinline__ int64_t start(int e, uint32_t c) const { return (int64_t)(c - first[e]) * kChunk; }
-  __device__ __forceinline__ int length(int e, uint32_t c) const { return c + 1 == first[e + 1] ? src[e].tail() : (int)kChunk; }
+  __device__ __forceinline__ int64_t start(int e, uint32_t c) const { return (int64_t)(c - first[e]) * chunk_elements(src[e].f32()); }
+  __device__ __forceinline__ int length(int e, uint32_t c) const {
+    return c + 1 == first[e + 1] ? src[e].tail() : (int)chunk_elements(src[e].f32());
+  }
 };
 
 // Lists of this many bytes or more are past the 256 MB last-level cache: streamed
 // (non-temporal) accesses are faster there.  534M fp32 elements: the norm 354 us
-// without, 314 (6.8 TB/s) with; clipped into bf16, loads and stores, 586 and 545
-// (5.9 TB/s).  200 MB: no difference.
+// without, 314 (6.8 TB/s) with; clipped into bf16 in chunks of 64 KB, loads and
+// stores, 586 and 545 (515 in chunks of 32 KB, 6.2 TB/s).  200 MB: no difference.
 constexpr int64_t kStreamBytes = int64_t(256) << 20;
 
 template <bool NT, typename V>
@@ -308,8 +313,8 @@ static int fill_table(const bgpo_tensor* g, const bgpo_tensor* out, int32_t coun
   uint32_t chunks = 0;
   for (; at < count && t->count < N; ++at) {
     if (!g[at].n) continue;
-    const int64_t more = (g[at].n + kChunk - 1) / kChunk;
-    if (chunks + more > INT32_MAX) break;          // (2^24 at most for one: the first always fits)
+    const int64_t chunk = chunk_elements(g[at].dtype == BGPO_F32), more = (g[at].n + chunk - 1) / chunk;
+    if (chunks + more > INT32_MAX) break;          // (2^25 at most for one: the first always fits)
     const int k = t->count++;
     t->src[k] = Packed::of(g[at]);
     if (OUT) t->dst[k] = Packed::of(out[at]);
