@@ -405,3 +405,36 @@ def test_long_rows_by_where_they_count(where):
             a[k] = np.where(a["lose_mask"] == 0, np.float32(np.nan), np.nan_to_num(a[k], nan=-1.5)).astype(np.float32)
         for mean in (False, True):
             _check_pref(a, torch.float32, pad=1, kind="sigmoid", mean=mean)
+
+
+@pytest.mark.parametrize("L", [40, 700, 4099])
+def test_rows_far_apart(L):
+    """Responses more than 2^32 bytes apart, and beyond 2^31 elements: the bits of
+    the same responses packed."""
+    b = lib()
+    B, ld = 3, (1 << 30) + 3
+    g = torch.Generator(device="cuda").manual_seed(L)
+    r = lambda: -torch.randn(B, L, generator=g, device="cuda").abs()  # noqa: E731
+    lp, old = r(), r()
+    adv = torch.randn(B, generator=g, device="cuda")
+    mask = torch.rand(B, L, generator=g, device="cuda") < 0.8
+    big, big_out = (torch.empty((B - 1) * ld + L, device="cuda") for _ in range(2))
+    far, out = (torch.as_strided(t, (B, L), (ld, 1)) for t in (big, big_out))
+    far.copy_(lp)
+    prob = b.PolicyLoss(B, L, ratio=b.BGPO_RATIO_SEQUENCE, reduce=b.BGPO_REDUCE_RESPONSES)
+    ws = b.policy_workspace(prob)
+    res = []
+    for x, d in ((lp, torch.empty_like(lp)), (far, out)):
+        stats = torch.empty(6, dtype=torch.float64, device="cuda")
+        b.bgpo_policy_loss(prob, x, old, None, adv, mask, d, stats, ws)
+        res.append((stats.cpu(), d.contiguous().cpu()))
+    assert torch.equal(res[0][0], res[1][0]) and torch.equal(res[0][1], res[1][1])
+    pref = b.PreferenceLoss(B, L)
+    ws = b.preference_workspace(pref)
+    res = []
+    for x, d in ((lp, torch.empty_like(lp)), (far, out)):
+        stats = torch.empty(3, dtype=torch.float64, device="cuda")
+        dlo = torch.empty_like(old)
+        b.bgpo_preference_loss(pref, x, old, None, None, mask, mask, d, dlo, None, None, None, stats, ws)
+        res.append((stats.cpu(), d.contiguous().cpu(), dlo.cpu()))
+    assert all(torch.equal(p, q) for p, q in zip(*res))

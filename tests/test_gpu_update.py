@@ -174,3 +174,57 @@ def test_elbo_update_matches_the_oracle(kind):
     for o, t in zip(outs, (r.dX, r.dW)):
         v = t * (max_norm / want)
         assert np.abs(o.double().cpu().numpy() - v).max() <= 2.5e-2 * np.abs(v).max()
+
+
+def _independent_calls(b, seed):
+    """Every operator on inputs, outputs and workspaces of its own; (call, outputs)."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    r = lambda *s, **k: torch.randn(*s, generator=g, device="cuda", **k)  # noqa: E731
+    rows, V, B, L, P = 96, 20011, 300, 3001, 64
+    f = lambda n, t=torch.float32: torch.empty(n, dtype=t, device="cuda")  # noqa: E731
+    x = r(rows, V).bfloat16()
+    y = torch.randint(0, V, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    logp, ent, lse, a = f(rows), f(rows), f(rows), r(rows)
+    dx, lws = torch.empty_like(x), b.logits_workspace(rows, V)
+    lp, old, ref, adv = -r(B, L).abs(), -r(B, L).abs(), -r(B, L).abs(), r(B)
+    mask = torch.rand(B, L, generator=g, device="cuda") < 0.7
+    prob, dl, stats = b.PolicyLoss(B, L, kl_coef=0.1), torch.empty_like(lp), f(6, torch.float64)
+    pws = b.policy_workspace(prob)
+    pref, dw, dlo, pstats = b.PreferenceLoss(P, L, loss_scale=1 / P), torch.empty_like(lp[:P]), torch.empty_like(lp[:P]), f(3, torch.float64)
+    prefws = b.preference_workspace(pref)
+    grads, norm, gws = [r(100003), r(77, 501).bfloat16(), r(1 << 20)], f(1, torch.float64), b.grad_workspace()
+    outs = [torch.empty_like(t, dtype=torch.bfloat16) for t in grads]
+    gl, ol = b.GradList(grads), b.GradList(outs)
+
+    def call(s):
+        b.bgpo_logits_logp(x, y, logp, ent, lse, lws, stream=s)
+        b.bgpo_logits_logp_bwd(x, y, lse, ent, a, a, dx, stream=s)
+        b.bgpo_policy_loss(prob, lp, old, ref, adv, mask, dl, stats, pws, stream=s)
+        b.bgpo_preference_loss(pref, lp[:P], lp[P:2 * P], old[:P], old[P:2 * P], mask[:P], mask[P:2 * P], dw, dlo, None, None, None,
+                               pstats, prefws, stream=s)
+        b.bgpo_grad_norm(gl, norm, gws, stream=s)
+        b.bgpo_grad_clip(gl, 3.0, norm, ol, stream=s)
+
+    return call, [logp, ent, lse, dx, dl, stats, dw, dlo, pstats, norm] + outs
+
+
+def test_calls_on_two_streams_at_once():
+    """With workspaces of their own, the bits of calls one after the other."""
+    b = lib()
+    calls = [_independent_calls(b, seed) for seed in (1, 2)]
+    want = []
+    for call, outs in calls:
+        call(None)
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in outs])
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(3):
+        for _, outs in calls:
+            for t in outs:
+                t.fill_(7.0)
+        torch.cuda.synchronize()
+        for (call, _), s in zip(calls, streams):
+            call(s)
+        torch.cuda.synchronize()
+        for (_, outs), w in zip(calls, want):
+            assert all(torch.equal(t, v) for t, v in zip(outs, w))
